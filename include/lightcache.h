@@ -520,6 +520,123 @@ lc_status lc_unet_cache_write(lc_unet* ctx, int dev_slot, const void* deep /* [d
 lc_status lc_unet_cache_peek(lc_unet* ctx, int host_slot, const void** ptr /* [host] */, size_t* bytes);
 lc_status lc_unet_cache_dev_peek(lc_unet* ctx, int dev_slot, const void** ptr /* [device] */, size_t* bytes);
 
+/* ---- operators over the tokens of long videos ----------------------------------------------------------------
+ * What a diffusion transformer needs beside the block stack above once its videos get long: rotary positions of the
+ * queries and keys, attention over the key blocks that a cheap score selects, and cache entries that are quantised as
+ * they are written and read back. They take their shapes from a descriptor and need no context.
+ *   - stream: hipStream_t of the device that is current, NULL being its default stream. Calls only enqueue kernels on it:
+ *     they allocate nothing, do not synchronise and may be captured into a graph. Every pointer must belong to that device.
+ *   - Errors: lc_status; the message is lc_last_error(NULL) of the calling thread. A refused call has launched nothing.
+ *   - Tensors [B, T, heads, head_dim] are given by a pointer to their first element and the strides of their first three
+ *     axes in elements (channels lie next to each other): rows of packed q,k,v, heads in front of tokens and tensors that one
+ *     batch element shares (stride 0, inputs only) are all of this form. Elements are of `dtype` (lc_dtype).
+ *   - Lengths q_len, k_len [device, int32, B] or NULL: of batch element b only the first q_len[b] queries / k_len[b] keys
+ *     exist (values are clamped to [0, Tq] / [0, Tk]). What lies behind is never read; rows of outputs behind q_len[b] are
+ *     left as they were. */
+typedef struct lc_strides { int64_t batch, token, head; } lc_strides;
+
+/* Rotary positions. The first rot_dim = axis_dim[0] + .. channels of a head are pairs (u, v), which a token at position p
+ * turns by the angle p w:  (u, v) -> A (u cos - v sin, u sin + v cos); the channels behind them stay. Axis a owns axis_dim[a]
+ * channels (those of axis 0 first) and a position of its own (a frame and a place in it, say); pair i of its D = axis_dim[a]
+ * has w = base^(-2 i / D) and is, counted from the axis's first channel,
+ *   LC_ROPE_HALF (i, i + D / 2)        LC_ROPE_INTERLEAVED (2 i, 2 i + 1).
+ * Scaling for positions beyond the length that a model was made for (orig_len), by a factor s > 0:
+ *   LC_ROPE_LINEAR w / s        LC_ROPE_BASE base s^(D / (D - 2)) in place of base, where D > 2
+ *   LC_ROPE_PARTS  w (g + (1 - g) / s), g = clamp((r - beta_slow) / (beta_fast - beta_slow), 0, 1), where r = orig_len w / 2 pi is how often
+ *                  the pair turns within orig_len, and A = 0.1 ln s + 1 where s > 1. Otherwise A = 1.
+ * Angles are formed in 64 bits whatever the type, so that positions in the millions lose nothing; the rotation is fp32. */
+typedef enum { LC_ROPE_HALF = 0, LC_ROPE_INTERLEAVED = 1 } lc_rope_layout;
+typedef enum { LC_ROPE_UNSCALED = 0, LC_ROPE_LINEAR = 1, LC_ROPE_BASE = 2, LC_ROPE_PARTS = 3 } lc_rope_scaling;
+#define LC_ROPE_MAX_PAIRS 64
+typedef struct lc_rope_config {
+  int32_t head_dim, axes;  /* 2 .. 128; 1 .. 3 */
+  int32_t axis_dim[3];     /* even, > 0 for the first `axes` of them; their sum at most head_dim */
+  int32_t layout, scaling, orig_len; /* orig_len: LC_ROPE_PARTS only */
+  double base, factor;     /* base > 1; factor > 0 */
+  double beta_fast, beta_slow; /* LC_ROPE_PARTS only, beta_fast > beta_slow (32 and 1 are usual) */
+} lc_rope_config;
+/* What lc_rope_make works out once for a model; plain data, copied by the calls that take it. */
+typedef struct lc_rope_table {
+  int32_t head_dim, rot_dim, axes, layout;
+  int32_t axis_dim[3];
+  int32_t checked;         /* set by lc_rope_make */
+  double amplitude;
+  double turns[LC_ROPE_MAX_PAIRS]; /* per pair, w / 2 pi */
+} lc_rope_table;
+lc_status lc_rope_make(const lc_rope_config* cfg, lc_rope_table* out /* [host] */); /* host only */
+typedef struct lc_rope_args {
+  int32_t B, T, heads, dtype;
+  lc_strides x, y;
+  int32_t inverse;         /* 1: by the negative angle: the transpose of the map, what a gradient takes */
+  int32_t grid[3];         /* without pos: token t is the cell t of a grid in row-major order, axis a of which has grid[a] cells
+                              (the first axis may be exceeded); one axis needs no grid */
+  int64_t start[3];        /* without pos: added to every token's position, |start| < 2^40 */
+  int64_t pos_batch;       /* with pos: elements from one batch element's positions to the next's, 0 = shared */
+} lc_rope_args;
+/* y = rotated x. pos [device, int32, .. T x axes] or NULL: the positions, where they are not the cells of a grid. y may be x
+ * (with its strides); otherwise the two must not overlap. Any strides and alignment are taken; heads of whole 16-byte packets, 16-byte
+ * aligned, move in packets. */
+lc_status lc_op_rope(const lc_rope_table* table /* [host] */, const lc_rope_args* args /* [host] */, const void* x, const int32_t* pos,
+                     void* y, void* stream);
+
+/* Attention over selected blocks. The keys are cut into blocks of `block` tokens, the queries into groups of q_block that share
+ * a list of key blocks (q_block = 1: every query has its own). A block's score for a group is the product of the means of
+ * the group's queries and of the block's keys; a list holds the `keep` blocks of the highest scores. Query head h reads key
+ * head h / (heads / kv_heads).
+ * Requirements (else LC_ERR_SHAPE): sizes > 0; heads a multiple of kv_heads; head_dim in {8, 16, 32, 40, 64, 128}; block a
+ * multiple of 64; 1 <= q_block <= 128; keep <= 65536; at most 8192 blocks; strides and pointers of q, k, v and out such that every
+ * head's row is 16-byte aligned; 64 token strides of k and v within 2^30 bytes. */
+typedef struct lc_sparse_args {
+  int32_t B, Tq, Tk, heads, kv_heads, head_dim, dtype;
+  int32_t block, q_block, keep;
+  int32_t sink, window;    /* selection: blocks that every list holds: the first `sink` ones, and those that hold or are at most
+                              `window` away from a block that holds the positions of the group's queries (window < 0: none) */
+  int64_t q_pos0;          /* position of the first query among the keys */
+  int32_t q_prescaled;     /* attention: 1 = q holds Q * log2(e) / sqrt(head_dim), as the projections of the steps write it */
+  lc_strides q, k, v, out;
+} lc_sparse_args;
+int32_t lc_sparse_groups(const lc_sparse_args* args); /* groups of queries: ceil(Tq / q_block) */
+int32_t lc_sparse_blocks(const lc_sparse_args* args); /* blocks of keys: ceil(Tk / block) */
+/* means[b][kv head][channel][block] = mean of the block's existing keys (0 where none exists), for the blocks [first, first +
+ * count): a cache that grows has only its last blocks done again. [device, double, B x kv_heads x head_dim x lc_sparse_blocks].
+ * Kept in 64 bits, as the scores are: the order of two blocks then depends on the keys, not on the order of a sum. */
+lc_status lc_op_block_means(const lc_sparse_args* args, const void* k, const int32_t* k_len, double* means, int first, int count,
+                            void* stream);
+/* index[b][head][group][keep] [device, int32]: the group's blocks, ascending, -1 behind the last. Blocks without an existing key are
+ * never listed, nor is anything for a group without an existing query. Forced blocks come first (the lowest ones if `keep` does not
+ * hold them all), then the highest scores, equal ones by the lower index; a score that is not a number ranks last. */
+lc_status lc_op_block_select(const lc_sparse_args* args, const void* q, const double* means, const int32_t* q_len, const int32_t* k_len,
+                             int32_t* index, void* stream);
+/* out[b][i][h] = softmax(q_i K^T / sqrt(head_dim)) V over the existing keys of the blocks in index[b][h][i / q_block]; zeros where
+ * there are none. A list ends at its first entry that is not a block with an existing key or not greater than the entry
+ * before it, so that lists of any origin are safe and no key counts twice. workspace [device, 16-byte aligned], of
+ * lc_block_attention_workspace(args) bytes (0: may be NULL): what several workgroups that share a list hand to each other; calls in
+ * flight at once need one each. */
+size_t lc_block_attention_workspace(const lc_sparse_args* args); /* host only; 0 also if args are refused */
+lc_status lc_op_block_attention(const lc_sparse_args* args, const void* q, const void* k, const void* v, const int32_t* index,
+                                const int32_t* q_len, const int32_t* k_len, void* out, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* Quantised cache entries. An entry holds rows of `cols` values in groups of 32 (the last of a row may be shorter) that share a
+ * scale 2^e: e is the least integer, at least -127, with max |x| <= M 2^e, so that nothing saturates, and a value is stored as the code
+ * nearest to x 2^-e (ties to even):
+ *   LC_ENTRY_INT8  integers, M = 127        LC_ENTRY_FP8  e4m3, M = 448        LC_ENTRY_FP4  e2m1, M = 6 (the first of two in the low bits)
+ * Scales are bytes e + 127. A group that holds an infinity or a NaN is marked by the byte 255 and reads back as NaN. Codes
+ * come first, rows of ceil(cols / 32) * 32 (zeros behind the last column), then the scale bytes, ceil(cols / 32) a row. */
+typedef enum { LC_ENTRY_PLAIN = -1, LC_ENTRY_INT8 = 0, LC_ENTRY_FP8 = 1, LC_ENTRY_FP4 = 2 } lc_entry_format;
+typedef struct lc_entry_args {
+  int32_t format;          /* lc_entry_format, not LC_ENTRY_PLAIN */
+  int32_t cols;
+  int64_t rows;
+  int32_t x_dtype, y_dtype; /* lc_dtype of x; of base and y */
+  int64_t x_ld, y_ld;      /* elements from one row to the next: of x; of base and y */
+} lc_entry_args;
+size_t lc_entry_packed_bytes(const lc_entry_args* args); /* host only; 0 if format or sizes are refused */
+/* Writes the entry [device, 16-byte aligned] of x; with y also y = base + what the entry now stands for, in the same pass (base NULL:
+ * zeros; base may be y, and x may be base or y). lc_op_entry_unpack reads it back: y = base + values. */
+lc_status lc_op_entry_pack(const lc_entry_args* args, const void* x, void* entry, const void* base, void* y, void* stream);
+lc_status lc_op_entry_unpack(const lc_entry_args* args, const void* entry, const void* base, void* y, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -128,6 +128,42 @@ class lc_unet_weights(C.Structure):
                 ("out", lc_unet_conv_w)]
 
 
+LC_ROPE_HALF, LC_ROPE_INTERLEAVED = 0, 1
+LC_ROPE_UNSCALED, LC_ROPE_LINEAR, LC_ROPE_BASE, LC_ROPE_PARTS = range(4)
+LC_ROPE_MAX_PAIRS = 64
+LC_ENTRY_PLAIN, LC_ENTRY_INT8, LC_ENTRY_FP8, LC_ENTRY_FP4 = -1, 0, 1, 2
+
+
+class lc_strides(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("batch", "token", "head")]
+
+
+class lc_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("axes", C.c_int32), ("axis_dim", C.c_int32 * 3), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("orig_len", C.c_int32)] + [(n, C.c_double) for n in ("base", "factor", "beta_fast", "beta_slow")]
+
+
+class lc_rope_table(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("head_dim", "rot_dim", "axes", "layout")] + \
+               [("axis_dim", C.c_int32 * 3), ("checked", C.c_int32), ("amplitude", C.c_double), ("turns", C.c_double * LC_ROPE_MAX_PAIRS)]
+
+
+class lc_rope_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "T", "heads", "dtype")] + [("x", lc_strides), ("y", lc_strides), ("inverse", C.c_int32),
+                ("grid", C.c_int32 * 3), ("start", C.c_int64 * 3), ("pos_batch", C.c_int64)]
+
+
+class lc_sparse_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Tq", "Tk", "heads", "kv_heads", "head_dim", "dtype", "block", "q_block", "keep", "sink",
+                                         "window")] + \
+               [("q_pos0", C.c_int64), ("q_prescaled", C.c_int32)] + [(n, lc_strides) for n in ("q", "k", "v", "out")]
+
+
+class lc_entry_args(C.Structure):
+    _fields_ = [("format", C.c_int32), ("cols", C.c_int32), ("rows", C.c_int64), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32),
+                ("x_ld", C.c_int64), ("y_ld", C.c_int64)]
+
+
 # name -> (restype, argtypes). Every symbol include/lightcache.h declares is listed here.
 _P, _I, _I64 = C.c_void_p, C.c_int, C.c_int64
 PROTOTYPES = {
@@ -216,6 +252,17 @@ PROTOTYPES = {
     "lc_op_down_conv": (_I, [_P, _P, _P, _I]),
     "lc_op_up_conv": (_I, [_P, _P, _P, _P, _I]),
     "lc_op_conv_out": (_I, [_P, _P, _P, _I]),
+    "lc_rope_make": (_I, [C.POINTER(lc_rope_config), C.POINTER(lc_rope_table)]),
+    "lc_op_rope": (_I, [C.POINTER(lc_rope_table), C.POINTER(lc_rope_args), _P, _P, _P, _P]),
+    "lc_sparse_groups": (C.c_int32, [C.POINTER(lc_sparse_args)]),
+    "lc_sparse_blocks": (C.c_int32, [C.POINTER(lc_sparse_args)]),
+    "lc_op_block_means": (_I, [C.POINTER(lc_sparse_args), _P, _P, _P, _I, _I, _P]),
+    "lc_op_block_select": (_I, [C.POINTER(lc_sparse_args), _P, _P, _P, _P, _P, _P]),
+    "lc_block_attention_workspace": (C.c_size_t, [C.POINTER(lc_sparse_args)]),
+    "lc_op_block_attention": (_I, [C.POINTER(lc_sparse_args), _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "lc_entry_packed_bytes": (C.c_size_t, [C.POINTER(lc_entry_args)]),
+    "lc_op_entry_pack": (_I, [C.POINTER(lc_entry_args), _P, _P, _P, _P, _P]),
+    "lc_op_entry_unpack": (_I, [C.POINTER(lc_entry_args), _P, _P, _P, _P]),
 }
 
 _lib: Optional[C.CDLL] = None
@@ -421,6 +468,55 @@ def lc_op_up_conv(ctx, skip_ptr, deep_ptr, u_ptr, frames) -> None:
 
 def lc_op_conv_out(ctx, u_ptr, eps_ptr, frames) -> None:
     _check(lib().lc_op_conv_out(ctx, u_ptr, eps_ptr, frames), ctx)
+
+
+# ---- operators over the tokens of long videos (no context; `stream`: a hipStream_t of the current device) --------------
+def lc_rope_make(cfg: lc_rope_config) -> lc_rope_table:
+    out = lc_rope_table()
+    _check(lib().lc_rope_make(C.byref(cfg), C.byref(out)), None)
+    return out
+
+
+def lc_op_rope(table: lc_rope_table, args: lc_rope_args, x_ptr, pos_ptr, y_ptr, stream) -> None:
+    _check(lib().lc_op_rope(C.byref(table), C.byref(args), x_ptr, pos_ptr, y_ptr, stream), None)
+
+
+def lc_sparse_groups(args: lc_sparse_args) -> int:
+    return lib().lc_sparse_groups(C.byref(args))
+
+
+def lc_sparse_blocks(args: lc_sparse_args) -> int:
+    return lib().lc_sparse_blocks(C.byref(args))
+
+
+def lc_op_block_means(args: lc_sparse_args, k_ptr, k_len_ptr, means_ptr, first: int, count: int, stream) -> None:
+    _check(lib().lc_op_block_means(C.byref(args), k_ptr, k_len_ptr, means_ptr, first, count, stream), None)
+
+
+def lc_op_block_select(args: lc_sparse_args, q_ptr, means_ptr, q_len_ptr, k_len_ptr, index_ptr, stream) -> None:
+    _check(lib().lc_op_block_select(C.byref(args), q_ptr, means_ptr, q_len_ptr, k_len_ptr, index_ptr, stream), None)
+
+
+def lc_block_attention_workspace(args: lc_sparse_args) -> int:
+    return lib().lc_block_attention_workspace(C.byref(args))
+
+
+def lc_op_block_attention(args: lc_sparse_args, q_ptr, k_ptr, v_ptr, index_ptr, q_len_ptr, k_len_ptr, out_ptr, workspace_ptr,
+                          workspace_bytes: int, stream) -> None:
+    _check(lib().lc_op_block_attention(C.byref(args), q_ptr, k_ptr, v_ptr, index_ptr, q_len_ptr, k_len_ptr, out_ptr, workspace_ptr,
+                                       workspace_bytes, stream), None)
+
+
+def lc_entry_packed_bytes(args: lc_entry_args) -> int:
+    return lib().lc_entry_packed_bytes(C.byref(args))
+
+
+def lc_op_entry_pack(args: lc_entry_args, x_ptr, entry_ptr, base_ptr, y_ptr, stream) -> None:
+    _check(lib().lc_op_entry_pack(C.byref(args), x_ptr, entry_ptr, base_ptr, y_ptr, stream), None)
+
+
+def lc_op_entry_unpack(args: lc_entry_args, entry_ptr, base_ptr, y_ptr, stream) -> None:
+    _check(lib().lc_op_entry_unpack(C.byref(args), entry_ptr, base_ptr, y_ptr, stream), None)
 
 
 # ---- sliced decoding ---------------------------------------------------------------------------

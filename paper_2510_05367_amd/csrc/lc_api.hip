@@ -845,6 +845,21 @@ lc_status op_checks(lc_ctx* c, int frames) {
 
 }  // namespace
 
+namespace lc {
+int op_fail(int status, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    g_err = buf;
+  } catch (...) {  // (no memory for the message: the status says it)
+  }
+  return status;
+}
+}  // namespace lc
+
 // =================================================================================================
 extern "C" {
 

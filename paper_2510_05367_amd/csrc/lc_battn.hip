@@ -1,0 +1,546 @@
+// Attention over listed key blocks.
+//
+// A workgroup owns one group of queries of one (batch element, head) and walks the 64-key chunks of the blocks that the
+// group has listed, keeping per query the running maximum and sum of its softmax, so that no score leaves the registers. Scores are
+// formed transposed, S^T[key][query] = K Q^T in 32 x 32 tiles: a lane then holds 16 keys of one query, the statistics are in-lane
+// but for one exchange, and the probabilities, rounded to the operands' type, are the B operand of O^T[dim][query] += V^T P^T as they
+// are. K and V rows go from memory straight into LDS, 16 bytes a lane, through buffer descriptors whose range check
+// delivers zeros for the keys beyond the sequence; the transposed V operand is read out of the rows with the
+// transposing LDS read (bf16), so no transposed copy of V exists anywhere.
+#include <atomic>
+
+#include "../../include/lightcache.h"
+#include "lc_internal.h"
+
+namespace lc {
+
+int check_sparse_args(const lc_sparse_args* a);  // lc_tokens.hip
+int check_sparse_rows(const char* name, const void* p, const lc_strides& s, int dt);
+
+namespace {
+
+constexpr int kRawBuffer = 0x00020000;  // resource word 3: raw 32-bit data
+typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+struct BlockAttnArgs {
+  lc_strides qs, ks, vs, os;
+  const int32_t *index, *q_len, *k_len;
+  float* part;      // several workgroups a list: [query of all][split][D] sums, then [query of all][split][2] maxima and denominators
+  float scale;      // of a score, to log2 units
+  int B, Tq, Tk, H, Hkv, block, q_block, keep, nq, splits;
+};
+
+// KS: wavefronts that share a tile of 32 queries and take turns at its keys. 1: four tiles (groups of up to 128 queries), every
+// wavefront takes both halves of a chunk; 2: two tiles, a half each; 4: one tile, and two chunks at a time.
+template <class T, int D, int KS> struct BlockAttnShape {
+  static constexpr int VEC = Vec16<T>::N;
+  static constexpr int PK = D / VEC;             // 16-byte packets of a row
+  static constexpr int KP = (PK + 1) / 2 * 2;    // ... in LDS, those beyond D being zeros
+  static constexpr int DM = (D + 31) / 32;       // 32-row tiles of O^T
+  static constexpr int TILE = 64 * KP * 16;      // bytes of a chunk's K rows, or of its V rows
+  static constexpr int NCH = KS == 4 && 2 * TILE <= 32768 ? 2 : 1;  // chunks of a stage
+  static constexpr int STAGE = NCH * 2 * TILE;
+  static constexpr int NB = STAGE <= 16384 ? 4 : 2;                 // stages in LDS
+  static constexpr int RED = KS == 1 ? 0 : 4 * (DM * 32 * 33 + 64) * 4;  // what wavefronts hand over at the end
+  static constexpr int LDS = NB * STAGE > RED ? NB * STAGE : RED;
+  static constexpr int LPW = NCH * KP / 2;       // loads of a stage that a wavefront issues
+};
+
+template <class T, int D, int KS>
+__global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, const T* __restrict__ q, const T* __restrict__ k,
+                                                            const T* __restrict__ v, T* __restrict__ out) {
+  typedef BlockAttnShape<T, D, KS> S;
+  typedef Mma32<T> M;
+  constexpr int VEC = S::VEC, PK = S::PK, KP = S::KP, DM = S::DM, NCH = S::NCH, NB = S::NB, LPW = S::LPW;
+  constexpr int KT = KS == 1 ? 2 : 1;      // 32-key sub-tiles of a stage and wavefront
+  constexpr int STEPS = KP / 2;            // packets a lane contracts along d
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr bool POW2 = (KP & (KP - 1)) == 0;
+  constexpr int PD = NB - 1;               // stages in flight
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  int* const n_list = reinterpret_cast<int*>(smem);  // (before the first stage lands there)
+
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, hh = lane >> 5;
+  // all groups of a (batch element, head) on one XCD, whose L2 then fetches its keys and values once
+  int prob, in;
+  {
+    const int per = a.nq * a.splits, nprob = a.B * a.H, id = blockIdx.x;
+    if (nprob % 8 == 0) {
+      const int slot = id >> 3, p8 = slot / per;
+      prob = (id & 7) + 8 * p8;
+      in = slot - p8 * per;
+    } else {
+      prob = id / per;
+      in = id - prob * per;
+    }
+  }
+  const int split = in % a.splits, g = in / a.splits, b = prob / a.H, h = prob - b * a.H, hk = h / (a.H / a.Hkv);
+  const int TK = a.k_len ? min(max(a.k_len[b], 0), a.Tk) : a.Tk;
+  const int row0 = g * a.q_block, rows = min(min(a.q_len ? max(a.q_len[b], 0) : a.Tq, a.Tq) - row0, a.q_block);
+  if (rows <= 0) return;
+  const int32_t* const list = a.index + ((int64_t)prob * a.nq + g) * a.keep;
+
+  // ---- queries: B operand of S^T = K Q^T; packets beyond D and rows beyond the group are zeros
+  const int tile = KS == 1 ? wid : KS == 2 ? wid >> 1 : 0;
+  const int qi = tile * 32 + lq;
+  Vec16<T> qf[STEPS];
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int pk = 2 * j + hh;
+    qf[j] = qi < rows && pk < PK ? load16(q + b * a.qs.batch + (int64_t)(row0 + qi) * a.qs.token + h * a.qs.head + pk * VEC) : zero16<T>();
+  }
+
+  // the list ends before its first entry that is no existing block or does not ascend
+  if (tid == 0) *n_list = a.keep;
+  __syncthreads();
+  for (int i = tid; i < a.keep; i += 256) {
+    const int e = list[i];
+    if (e < 0 || (int64_t)e * a.block >= TK || (i > 0 && e <= list[i - 1])) atomicMin(n_list, i);
+  }
+  __syncthreads();
+  const int cpb = a.block / 64;
+  const int chunks = __builtin_amdgcn_readfirstlane(*n_list) * cpb;
+  const int c_lo = (int)((int64_t)chunks * split / a.splits), c_hi = (int)((int64_t)chunks * (split + 1) / a.splits);
+  const int nstage = (c_hi - c_lo + NCH - 1) / NCH;
+  __syncthreads();
+
+  // ---- what this wavefront moves: K or V rows of one chunk of a stage, or half of them
+  const int my_chunk = NCH == 2 ? wid >> 1 : 0;
+  const bool moves_v = NCH == 2 ? wid & 1 : wid >> 1;
+  const int first = NCH == 2 ? 0 : (wid & 1) * LPW;  // load of the tile
+  const int64_t ld = moves_v ? a.vs.token : a.ks.token;
+  const T* const src = moves_v ? v + b * a.vs.batch + hk * a.vs.head : k + b * a.ks.batch + hk * a.ks.head;
+  // 16-byte slots are swizzled so that what neighbouring lanes read together lies in different banks: K rows are read a
+  // slot of 32 rows at a time, V rows 64 bytes of four rows (bf16), or 128 bytes of a row and of the fourth behind it (float)
+  auto k_swz = [](int key) { return !POW2 ? 0 : KP >= 16 ? key & 15 : (key / (16 / KP)) & (KP - 1); };
+  auto v_swz = [](int key) {
+    if (BF) return KP == 8 ? ((key >> 1) & 1) * 4 : KP == 16 ? (key & 3) * 4 : 0;
+    return KP >= 16 ? ((key >> 2) & 1) * 8 : 0;
+  };
+  uint32_t off[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int p = (first + i) * 64 + lane, key = p / KP, c = (p - key * KP) ^ (moves_v ? v_swz(key) : k_swz(key));
+    off[i] = c < PK ? (uint32_t)(key * ld + c * VEC) * (uint32_t)sizeof(T) : 0x7fffff00u;
+  }
+  const unsigned lds_at = (my_chunk * 2 + (moves_v ? 1 : 0)) * S::TILE + first * 1024;
+  // The chunks of the list in turn, TK (no keys) behind the end: a lane holds an entry, 64 at a time
+  int at = c_lo + my_chunk, at_li = at / cpb, at_sub = at - at_li * cpb, held = at_li & ~63;
+  int ent = list[min(held + lane, a.keep - 1)];
+  // (everything loaded so far is waited for here, not where the loop uses it: the requests below must stay in flight)
+  asm volatile("" : "+v"(ent));
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) asm volatile("" : "+v"(qf[j].v));
+  auto next_key0 = [&]() {
+    if (at >= c_hi) return TK;
+    if (at_li - held >= 64) {
+      held = at_li & ~63;
+      ent = list[min(held + lane, a.keep - 1)];
+      asm volatile("" : "+v"(ent));
+    }
+    const int key0 = __builtin_amdgcn_readlane(ent, at_li & 63) * a.block + at_sub * 64;
+    at += NCH;
+    at_sub += NCH;
+    while (at_sub >= cpb) {
+      at_sub -= cpb;
+      ++at_li;
+    }
+    return key0;
+  };
+  // The requests are written out, so that the compiler does not take the transposing reads below to depend on all of them and
+  // waits for none: barrier_keep says when a stage is there. (No register is loaded, and what the descriptor is made of was written by scalar
+  // instructions; the first wait states are for those that were not.)
+  auto issue = [&](int st, int key0) {
+#ifdef __HIP_DEVICE_COMPILE__
+    const int keys = min(64, TK - key0);
+    const uint64_t base = (uint64_t)(src + key0 * ld);
+    typedef __attribute__((ext_vector_type(4))) int i32x4;
+    const i32x4 r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xffffu)),
+                     __builtin_amdgcn_readfirstlane(keys > 0 ? (int)(((keys - 1) * ld + D) * (int)sizeof(T)) : 0), kRawBuffer};
+    const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)(smem + (st % NB) * S::STAGE + lds_at));
+    asm volatile("s_nop 4" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < LPW; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst + i * 1024), "v"(off[i]), "s"(r) : "memory");
+#else
+    (void)st; (void)key0; (void)off; (void)lds_at; (void)src;
+#endif
+  };
+
+  const int half = KS == 1 ? 0 : wid & 1;          // of the chunk
+  const bool busy = KS != 4 || (wid >> 1) < NCH;   // (one chunk a stage leaves two of four wavefronts without keys)
+  const unsigned k_at = my_chunk * 2 * S::TILE + lq * (KP * 16), v_at = (my_chunk * 2 + 1) * S::TILE;
+  unsigned v_off[DM];
+  const int trow = BF ? (lane & 15) >> 2 : 0;
+#pragma unroll
+  for (int mt = 0; mt < DM; ++mt) {
+    if constexpr (BF) {  // 16 lanes read 16 dims of four keys: lane i four dims of key i / 4
+      const int dim = mt * 32 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3), slot = min(dim / 8, KP - 1);
+      v_off[mt] = (4 * hh + trow) * (KP * 16) + ((slot ^ v_swz(trow)) << 4) + (dim & 7) * 2;
+    } else {
+      const int dim = min(mt * 32 + lq, KP * VEC - 1);
+      v_off[mt] = 4 * hh * (KP * 16) + (((dim / 4) ^ v_swz(4 * hh)) << 4) + (dim & 3) * 4;
+    }
+  }
+
+  f32x16 o[DM];
+  float m = -INFINITY, l = 0.f;  // in log2 units: what the exponents subtract; this lane's part of the denominator
+#pragma unroll
+  for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[mt][r] = 0.f;
+
+  int k0[PD + 1];  // first keys of the stages in flight
+#pragma unroll
+  for (int s = 0; s < PD; ++s) {
+    k0[s] = next_key0();
+    issue(s, k0[s]);
+  }
+  for (int st = 0; st < nstage; ++st) {
+    // stage st has landed for everyone, and nobody still reads the buffer that the next request goes to. (Behind the last stage the
+    // requests deliver zeros: their number stays what the wait counts on.)
+    barrier_keep<(PD - 1) * LPW>();
+    k0[PD] = next_key0();
+    issue(st + PD, k0[PD]);
+    const unsigned char* const buf = smem + (st % NB) * S::STAGE;
+    const int key0 = k0[0] + half * 32;
+    if (busy && key0 < TK) {
+      f32x16 sc[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[kt][r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+          const Vec16<T> kf = *reinterpret_cast<const Vec16<T>*>(buf + k_at + (half + kt) * 32 * (KP * 16) + (((2 * j + hh) ^ k_swz(lq)) << 4));
+          if constexpr (BF) {
+            M::mma(kf.v, qf[j].v, sc[kt]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) M::mma(kf.v[e], qf[j].v[e], sc[kt]);
+          }
+        }
+      }
+      // lane holds keys key0 + 32 kt + 8 (r / 4) + 4 hh + r % 4 of query lq
+      if (k0[0] + 64 > TK) {
+        int kb = key0 + 4 * hh;
+        asm volatile("" : "+v"(kb));  // (left alone the compiler computes the indexes outside the branch)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (kb + kt * 32 + 8 * (r >> 2) + (r & 3) >= TK) sc[kt][r] = -INFINITY;
+      }
+      float mx = sc[0][0];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kt][r]);
+      mx *= a.scale;
+      // Any offset gives the same softmax while exp2 stays in range: it is raised, and what is summed up scaled, only when a score
+      // passes it by kLazy. Each query decides for itself, whoever shares its wavefront.
+      constexpr float kLazy = 8.f;
+      if (__builtin_amdgcn_ballot_w64(mx > m + kLazy) != 0) {
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = mx > m + kLazy ? mx : m;
+        const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[mt][r] *= alpha;
+      }
+      const float mc = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        if constexpr (BF) {
+          bf16x8 pf[2];
+#pragma unroll
+          for (int r = 0; r < 16; r += 2) {
+            bf16x2 p2, one2;
+            p2[0] = static_cast<bf16_t>(__builtin_amdgcn_exp2f(fmaf(sc[kt][r], a.scale, -mc)));
+            p2[1] = static_cast<bf16_t>(__builtin_amdgcn_exp2f(fmaf(sc[kt][r + 1], a.scale, -mc)));
+            pf[r / 8][r % 8] = p2[0];
+            pf[r / 8][r % 8 + 1] = p2[1];
+            one2[0] = one2[1] = (bf16_t)1.f;
+            // the denominator sums the probabilities as rounded: a key's share of numerator and denominator is then the same
+#ifdef __HIP_DEVICE_COMPILE__
+            l = __builtin_amdgcn_fdot2_f32_bf16(p2, one2, l, false);
+#endif
+          }
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int mt = 0; mt < DM; ++mt) {
+              bf16x8 vf = {};
+#ifdef __HIP_DEVICE_COMPILE__
+              typedef __attribute__((address_space(3))) s16x4* tr_ptr;
+              const unsigned char* const at = buf + v_at + v_off[mt] + ((half + kt) * 32 + 16 * s) * (KP * 16);
+              const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at));
+              const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 8 * (KP * 16)));
+              const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+              vf = __builtin_bit_cast(bf16x8, both);
+#else
+              (void)v_off;
+#endif
+              M::mma(vf, pf[s], o[mt]);
+            }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[kt][r], a.scale, -mc));
+            l += p;
+#pragma unroll
+            for (int mt = 0; mt < DM; ++mt) {
+              const float vf = *reinterpret_cast<const float*>(buf + v_at + v_off[mt] + ((half + kt) * 32 + 8 * (r >> 2) + (r & 3)) * (KP * 16));
+              M::mma(vf, p, o[mt]);
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < PD; ++s) k0[s] = k0[s + 1];
+  }
+  // (a wavefront must not end, nor the stages be used for anything else, with requests for them under way)
+  __builtin_amdgcn_s_waitcnt(waitcnt_imm(0));
+  l += __shfl_xor(l, 32, 64);
+
+  T* const ob = out + b * a.os.batch + h * a.os.head;
+  const int64_t pq = (int64_t)prob * a.Tq + row0;  // this group's first query, counted over all
+  float* const pml = a.part + (int64_t)a.B * a.H * a.Tq * a.splits * D;
+  if constexpr (KS == 1) {
+    if (qi >= rows) return;
+    if (a.splits > 1) {
+      float* const po = a.part + ((pq + qi) * a.splits + split) * D;
+#pragma unroll
+      for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+        for (int gr = 0; gr < 4; ++gr) {
+          const int dim = mt * 32 + 8 * gr + 4 * hh;
+          if (dim < D) *reinterpret_cast<f32x4*>(po + dim) = f32x4{o[mt][4 * gr], o[mt][4 * gr + 1], o[mt][4 * gr + 2], o[mt][4 * gr + 3]};
+        }
+      if (hh == 0) {
+        float* const w = pml + ((pq + qi) * a.splits + split) * 2;
+        w[0] = m;
+        w[1] = l;
+      }
+      return;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* const orow = ob + (int64_t)(row0 + qi) * a.os.token;
+#pragma unroll
+    for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr) {
+        const int dim = mt * 32 + 8 * gr + 4 * hh;
+        if (dim < D) {
+          if constexpr (BF) {
+            bf16x4 ov;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ov[e] = static_cast<bf16_t>(o[mt][4 * gr + e] * inv);
+            *reinterpret_cast<bf16x4*>(orow + dim) = ov;
+          } else {
+            *reinterpret_cast<f32x4*>(orow + dim) = f32x4{o[mt][4 * gr] * inv, o[mt][4 * gr + 1] * inv, o[mt][4 * gr + 2] * inv, o[mt][4 * gr + 3] * inv};
+          }
+        }
+      }
+  } else {
+    // ---- the wavefronts of a tile bring their sums to the largest of their offsets and add them, in a fixed order
+    barrier_keep<0>();
+    float* const red = reinterpret_cast<float*>(smem);  // [wavefront][dim][33]: O^T of the 32 queries
+    float* const ml = red + 4 * DM * 32 * 33;            // [wavefront][offset | denominator][32]
+    if (hh == 0) {
+      ml[wid * 64 + lq] = m;
+      ml[wid * 64 + 32 + lq] = l;
+    }
+    __syncthreads();
+    auto factor = [](float mw, float top) { return mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top); };
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < KS; ++w) top = fmaxf(top, ml[(tile * KS + w) * 64 + lq]);
+    const float f = factor(m, top);
+#pragma unroll
+    for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) red[((wid * DM + mt) * 32 + 8 * (r >> 2) + 4 * hh + (r & 3)) * 33 + lq] = o[mt][r] * f;
+    __syncthreads();
+    constexpr int QN = 128 / KS, TPQ = 256 / QN, ND = DM * 32 / TPQ;  // queries; threads a query; dims a thread
+    const int tq = tid / TPQ, td = tid % TPQ * ND, w0 = tq / 32 * KS, ql = tq & 31;
+    if (tq >= rows) return;
+    float lt = 0.f, mt_ = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < KS; ++w) mt_ = fmaxf(mt_, ml[(w0 + w) * 64 + ql]);
+#pragma unroll
+    for (int w = 0; w < KS; ++w) lt += ml[(w0 + w) * 64 + 32 + ql] * factor(ml[(w0 + w) * 64 + ql], mt_);
+    const bool whole = a.splits == 1;
+    const float inv = !whole ? 1.f : lt == 0.f ? 0.f : 1.f / lt;
+    T* const orow = ob + (int64_t)(row0 + tq) * a.os.token;
+    float* const po = a.part + ((pq + tq) * a.splits + split) * D;
+#pragma unroll
+    for (int e = 0; e < ND; e += 4) {
+      if (td + e < D) {
+        float s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[i] = 0.f;
+#pragma unroll
+          for (int w = 0; w < KS; ++w) s[i] += red[((w0 + w) * DM * 32 + td + e + i) * 33 + ql];
+        }
+        if (!whole) *reinterpret_cast<f32x4*>(po + td + e) = f32x4{s[0], s[1], s[2], s[3]};
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i) orow[td + e + i] = from_f32<T>(s[i] * inv);
+      }
+    }
+    if (!whole && td == 0) {
+      float* const w = pml + ((pq + tq) * a.splits + split) * 2;
+      w[0] = mt_;
+      w[1] = lt;
+    }
+  }
+}
+
+// out = the splits' sums brought to one offset, added in a fixed order and divided; a thread four dims of a query
+template <class T>
+__global__ __launch_bounds__(256) void block_attn_join_kernel(BlockAttnArgs a, T* __restrict__ out, int D) {
+  const int per = D / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.B * a.H * a.Tq;
+  const int64_t pq = i / per;
+  if (pq >= n) return;
+  const int dim = (int)(i - pq * per) * 4, prob = (int)(pq / a.Tq), row = (int)(pq - (int64_t)prob * a.Tq), b = prob / a.H, h = prob - b * a.H;
+  if (a.q_len && row >= a.q_len[b]) return;
+  const float* const ml = a.part + n * a.splits * D + pq * a.splits * 2;
+  const float* const po = a.part + pq * a.splits * D + dim;
+  float top = -INFINITY, l = 0.f;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[2 * s]);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s) {
+    const float f = ml[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2 * s] - top);
+    l += ml[2 * s + 1] * f;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[e], f, acc[e]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* const orow = out + b * a.os.batch + (int64_t)row * a.os.token + h * a.os.head + dim;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) orow[e] = from_f32<T>(acc[e] * inv);
+}
+
+int tiles_shared(const lc_sparse_args* a) {  // KS
+  const int rows = a->q_block < a->Tq ? a->q_block : a->Tq;
+  return rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+}
+// Workgroups that share a list: where there are too few groups for the chip, as many as leave each of them a few stages
+int list_splits(const lc_sparse_args* a) {
+  const int64_t groups = (int64_t)a->B * a->heads * lc_sparse_groups(a);
+  const int64_t cpb = a->block / 64, most = ((int64_t)a->Tk + 63) / 64;
+  const int64_t chunks = a->keep * cpb < most ? a->keep * cpb : most;
+  const int64_t stages = tiles_shared(a) == 4 ? (chunks + 1) / 2 : chunks;
+  if (groups >= 256) return 1;
+  const int64_t want = (512 + groups - 1) / groups, room = stages / 4;
+  const int64_t s = want < room ? want : room;
+  return s < 1 ? 1 : (int)s;
+}
+
+int check_attention(const lc_sparse_args* a) {
+  int s = check_sparse_args(a);
+  if (s != LC_OK) return s;
+  if (a->Tk > 1 << 30 || a->block > 1 << 20) return op_fail(LC_ERR_SHAPE, "Tk must be at most 2^30 and block at most 2^20");
+  const int64_t es = (int64_t)dtype_size(a->dtype), most = ((int64_t)1 << 30) / 64 / es;
+  if (a->k.token > most || a->v.token > most || a->k.token < 0 || a->v.token < 0) return op_fail(LC_ERR_SHAPE, "64 token strides of k and v must be within 2^30 bytes");
+  if (a->Tk > 1 && (a->k.token < a->head_dim || a->v.token < a->head_dim)) return op_fail(LC_ERR_SHAPE, "the rows of k and of v must not overlap");
+  const int64_t groups = (int64_t)a->B * a->heads * lc_sparse_groups(a);
+  if (groups > (int64_t)1 << 23) return op_fail(LC_ERR_SHAPE, "too many groups of queries");
+  return LC_OK;
+}
+
+template <class T, int D, int KS> hipError_t run_block_attn(hipStream_t s, const BlockAttnArgs& a, const void* q, const void* k, const void* v, void* out) {
+  constexpr int lds = BlockAttnShape<T, D, KS>::LDS;
+  static_assert(lds <= 160 * 1024, "fits a compute unit");
+  if (lds > 65536) {
+    static std::atomic<uint64_t> done{0};  // a bit for each device
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(done.load() & bit)) {
+      e = hipFuncSetAttribute((const void*)block_attn_kernel<T, D, KS>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e != hipSuccess) return e;
+      done.fetch_or(bit);
+    }
+  }
+  const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nq * a.splits);
+  block_attn_kernel<T, D, KS><<<grid, 256, lds, s>>>(a, (const T*)q, (const T*)k, (const T*)v, (T*)out);
+  return hipGetLastError();
+}
+template <class T> hipError_t block_attn_dispatch(hipStream_t s, const BlockAttnArgs& a, int d, int ks, const void* q, const void* k, const void* v, void* out) {
+#define LC_GO(D)                                              \
+  case D:                                                     \
+    return ks == 1 ? run_block_attn<T, D, 1>(s, a, q, k, v, out) \
+         : ks == 2 ? run_block_attn<T, D, 2>(s, a, q, k, v, out) \
+                   : run_block_attn<T, D, 4>(s, a, q, k, v, out)
+  switch (d) {
+    LC_GO(8);
+    LC_GO(16);
+    LC_GO(32);
+    LC_GO(40);
+    LC_GO(64);
+    LC_GO(128);
+    default: return hipErrorInvalidValue;
+  }
+#undef LC_GO
+}
+
+}  // namespace
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" {
+
+size_t lc_block_attention_workspace(const lc_sparse_args* a) {
+  if (check_attention(a) != LC_OK) return 0;
+  const int s = list_splits(a);
+  return s == 1 ? 0 : (size_t)a->B * a->heads * a->Tq * s * (a->head_dim + 2) * 4;
+}
+
+lc_status lc_op_block_attention(const lc_sparse_args* a, const void* q, const void* k, const void* v, const int32_t* index,
+                                const int32_t* q_len, const int32_t* k_len, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  int s = check_attention(a);
+  if (s == LC_OK) s = check_sparse_rows("q", q, a->q, a->dtype);
+  if (s == LC_OK) s = check_sparse_rows("k", k, a->k, a->dtype);
+  if (s == LC_OK) s = check_sparse_rows("v", v, a->v, a->dtype);
+  if (s == LC_OK) s = check_sparse_rows("out", out, a->out, a->dtype);
+  if (s != LC_OK) return (lc_status)s;
+  if (!index) return (lc_status)op_fail(LC_ERR_ARG, "index is NULL");
+  if (a->q_prescaled != 0 && a->q_prescaled != 1) return (lc_status)op_fail(LC_ERR_ARG, "q_prescaled must be 0 or 1");
+  const size_t need = lc_block_attention_workspace(a);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return (lc_status)op_fail(LC_ERR_NOMEM, "workspace of %zu bytes is smaller than the %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+  if (need > 0 && (uintptr_t)workspace % 16) return (lc_status)op_fail(LC_ERR_ARG, "workspace must be 16-byte aligned");
+  BlockAttnArgs k_;
+  k_.qs = a->q; k_.ks = a->k; k_.vs = a->v; k_.os = a->out;
+  k_.index = index; k_.q_len = q_len; k_.k_len = k_len;
+  k_.part = (float*)workspace;
+  k_.scale = a->q_prescaled ? 1.f : attn_q_scale(a->head_dim);
+  k_.B = a->B; k_.Tq = a->Tq; k_.Tk = a->Tk; k_.H = a->heads; k_.Hkv = a->kv_heads; k_.block = a->block; k_.q_block = a->q_block;
+  k_.keep = a->keep; k_.nq = lc_sparse_groups(a); k_.splits = list_splits(a);
+  const int ks = tiles_shared(a);
+  hipError_t e = a->dtype == LC_BF16 ? block_attn_dispatch<bf16_t>((hipStream_t)stream, k_, a->head_dim, ks, q, k, v, out)
+                                     : block_attn_dispatch<float>((hipStream_t)stream, k_, a->head_dim, ks, q, k, v, out);
+  if (e == hipSuccess && k_.splits > 1) {
+    const int64_t n = (int64_t)a->B * a->heads * a->Tq * (a->head_dim / 4);
+    const unsigned blocks = (unsigned)((n + 255) / 256);
+    if (a->dtype == LC_BF16) block_attn_join_kernel<bf16_t><<<blocks, 256, 0, (hipStream_t)stream>>>(k_, (bf16_t*)out, a->head_dim);
+    else block_attn_join_kernel<float><<<blocks, 256, 0, (hipStream_t)stream>>>(k_, (float*)out, a->head_dim);
+    e = hipGetLastError();
+  }
+  return e == hipSuccess ? LC_OK : (lc_status)op_fail(LC_ERR_HIP, "block_attention: %s", hipGetErrorString(e));
+}
+
+}  // extern "C"

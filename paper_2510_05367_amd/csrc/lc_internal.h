@@ -239,4 +239,8 @@ hipError_t launch_to_f32(hipStream_t s, int dt, const void* src, float* dst, int
 hipError_t launch_fill_f32(hipStream_t s, float* dst, int64_t n, float v);
 hipError_t launch_copy_rows(hipStream_t s, int dt, const void* src, void* dst, int64_t elems);
 
+// ---- operators without a context -------------------------------------------------------------
+// Leaves the message where lc_last_error(NULL) finds it and returns `status` (an lc_status); never throws.
+int op_fail(int status, const char* fmt, ...);
+
 }  // namespace lc
