@@ -637,6 +637,28 @@ size_t lc_entry_packed_bytes(const lc_entry_args* args); /* host only; 0 if form
 lc_status lc_op_entry_pack(const lc_entry_args* args, const void* x, void* entry, const void* base, void* y, void* stream);
 lc_status lc_op_entry_unpack(const lc_entry_args* args, const void* entry, const void* base, void* y, void* stream);
 
+/* ---- the diffusion-transformer variant on long videos: the operators above inside its steps ---------------------------------
+ * rope: the queries and keys of every block are turned by their tokens' cells in `grid` (axes as in lc_rope_args), behind the
+ * projection. keep > 0: attention over selected blocks in place of all tokens, the lists made anew in every block from its own
+ * queries and keys (tokens are positions: q_pos0 = 0). entry_format other than LC_ENTRY_PLAIN: Delta is quantised as a normal step
+ * or lc_dit_cache_write writes it; device slots, the pinned bank and the copies between them hold the entry of B*T rows of D values, and both
+ * kinds of step add what it stands for, so a cache step on the entry of the same input still reproduces the normal step
+ * bit for bit. */
+typedef struct lc_dit_options {
+  int32_t entry_format;             /* lc_entry_format */
+  int32_t keep, block, q_block, sink, window; /* as in lc_sparse_args; keep = 0: all tokens, the others unused */
+  const lc_rope_table* rope;        /* [host] or NULL: no positions; copied */
+  int32_t grid[3];
+} lc_dit_options;
+lc_status lc_dit_check_options(const lc_dit_config* cfg, const lc_dit_options* opt); /* host only */
+size_t lc_dit_options_entry_bytes(const lc_dit_config* cfg, const lc_dit_options* opt); /* host only; opt may be NULL: none */
+size_t lc_dit_options_workspace_bytes(const lc_dit_config* cfg, const lc_dit_options* opt, int token_chunk); /* host only; likewise */
+/* NULL: none, the state of a new context. Waits for both streams; every slot and bank entry becomes empty, and the bank is allocated
+ * anew where entries change their size. The workspace has to be handed over again if it is smaller than
+ * lc_dit_options_workspace_bytes (LC_ERR_NOMEM, as if the bank cannot be allocated: the options in force then stay, with all
+ * entries). */
+lc_status lc_dit_set_options(lc_dit* ctx, const lc_dit_options* opt);
+
 #ifdef __cplusplus
 }
 #endif

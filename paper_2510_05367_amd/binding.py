@@ -164,6 +164,11 @@ class lc_entry_args(C.Structure):
                 ("x_ld", C.c_int64), ("y_ld", C.c_int64)]
 
 
+class lc_dit_options(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("entry_format", "keep", "block", "q_block", "sink", "window")] + \
+               [("rope", C.POINTER(lc_rope_table)), ("grid", C.c_int32 * 3)]
+
+
 # name -> (restype, argtypes). Every symbol include/lightcache.h declares is listed here.
 _P, _I, _I64 = C.c_void_p, C.c_int, C.c_int64
 PROTOTYPES = {
@@ -225,6 +230,10 @@ PROTOTYPES = {
     "lc_dit_cache_peek": (_I, [_P, _I, C.POINTER(_P), C.POINTER(C.c_size_t)]),
     "lc_dit_cache_dev_peek": (_I, [_P, _I, C.POINTER(_P), C.POINTER(C.c_size_t)]),
     "lc_dit_get_counts": (_I, [_P] + [C.POINTER(C.c_int64)] * 4),
+    "lc_dit_check_options": (_I, [C.POINTER(lc_dit_config), C.POINTER(lc_dit_options)]),
+    "lc_dit_options_entry_bytes": (C.c_size_t, [C.POINTER(lc_dit_config), C.POINTER(lc_dit_options)]),
+    "lc_dit_options_workspace_bytes": (C.c_size_t, [C.POINTER(lc_dit_config), C.POINTER(lc_dit_options), _I]),
+    "lc_dit_set_options": (_I, [_P, C.POINTER(lc_dit_options)]),
     "lc_unet_check_config": (_I, [C.POINTER(lc_unet_config)]),
     "lc_unet_entry_bytes": (C.c_size_t, [C.POINTER(lc_unet_config)]),
     "lc_unet_workspace_bytes": (C.c_size_t, [C.POINTER(lc_unet_config)]),
@@ -738,6 +747,36 @@ def lc_dit_get_counts(ctx):
     return tuple(x.value for x in v)
 
 
+def make_dit_options(entry: Optional[str] = None, keep: int = 0, block: int = 64, q_block: int = 128, sink: int = 0, window: int = -1,
+                     rope: Optional[lc_rope_table] = None, grid=None) -> lc_dit_options:
+    """entry: None, "mxint8", "mxfp8" or "mxfp4"; keep = 0: attention over all tokens; rope: a table, with the grid its axes count in."""
+    formats = {None: LC_ENTRY_PLAIN, "mxint8": LC_ENTRY_INT8, "mxfp8": LC_ENTRY_FP8, "mxfp4": LC_ENTRY_FP4}
+    if entry not in formats:
+        raise ValueError("entry must be None, mxint8, mxfp8 or mxfp4")
+    return lc_dit_options(entry_format=formats[entry], keep=keep, block=block, q_block=q_block, sink=sink, window=window,
+                          rope=None if rope is None else C.pointer(rope), grid=(C.c_int32 * 3)(*(grid or [])))
+
+
+def lc_dit_check_options(cfg: lc_dit_config, opt: lc_dit_options) -> None:
+    _tcheck(lib().lc_dit_check_options(C.byref(cfg), C.byref(opt)), None)
+
+
+def _opt(opt: Optional[lc_dit_options]):
+    return None if opt is None else C.byref(opt)
+
+
+def lc_dit_options_entry_bytes(cfg: lc_dit_config, opt: Optional[lc_dit_options]) -> int:
+    return lib().lc_dit_options_entry_bytes(C.byref(cfg), _opt(opt))
+
+
+def lc_dit_options_workspace_bytes(cfg: lc_dit_config, opt: Optional[lc_dit_options], token_chunk: int) -> int:
+    return lib().lc_dit_options_workspace_bytes(C.byref(cfg), _opt(opt), token_chunk)
+
+
+def lc_dit_set_options(ctx, opt: Optional[lc_dit_options]) -> None:
+    _tcheck(lib().lc_dit_set_options(ctx, _opt(opt)), ctx)
+
+
 class Dit:
     """The block stack of the diffusion-transformer variant on the current GPU; torch owns memory and streams.
     `weights`: name -> numpy float32 array, names as in synth.dit_weight_manifest."""
@@ -765,6 +804,7 @@ class Dit:
         lc_dit_load_weights(self.ctx, w)
         del t
         self.arena = None
+        self.options: Optional[lc_dit_options] = None
         self._chunk = 0  # what a fresh context plans for: unchunked
         self.set_chunk(cfg.token_chunk if token_chunk is None else token_chunk)
 
@@ -777,8 +817,22 @@ class Dit:
         with self.torch.cuda.stream(self.compute):
             return self.torch.empty(*shape, dtype=self.torch.float32, device=self.device)
 
+    def set_options(self, options: Optional[lc_dit_options]) -> None:
+        """Options of :func:`make_dit_options` for the steps from here on (None: none). Empties every slot and bank entry."""
+        if options is not None:
+            lc_dit_check_options(self.ccfg, options)
+        need = lc_dit_options_workspace_bytes(self.ccfg, options, self._chunk)
+        if self.arena.numel() < need:
+            lc_dit_sync(self.ctx)
+            arena = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
+            self.torch.cuda.synchronize(self.device)
+            lc_dit_set_workspace(self.ctx, arena.data_ptr(), arena.numel())  # (also covers the options in force)
+            self.arena = arena
+        lc_dit_set_options(self.ctx, options)
+        self.options = options
+
     def set_chunk(self, token_chunk: int) -> None:
-        need = max(lc_dit_workspace_bytes(self.ccfg, token_chunk), lc_dit_workspace_bytes(self.ccfg, self._chunk))
+        need = max(lc_dit_options_workspace_bytes(self.ccfg, self.options, c) for c in (token_chunk, self._chunk))
         if self.arena is None or self.arena.numel() < need:
             # an arena that covers the plan in force and the new one (a new workspace starts with empty slots)
             lc_dit_sync(self.ctx)
@@ -812,11 +866,16 @@ class Dit:
         return C.string_at(ptr, n)
 
     def dev_entry(self, dev_slot: int):
-        """The Delta in a device slot as a float32 tensor [B, T, D] (a copy)."""
+        """The Delta in a device slot as a float32 tensor [B, T, D] (a copy; of a quantised entry what it stands for)."""
         ptr, n = lc_dit_cache_dev_peek(self.ctx, dev_slot)
         self.sync()
         off = ptr - self.arena.data_ptr()
         c = self.cfg
+        if self.options is not None and self.options.entry_format != LC_ENTRY_PLAIN:
+            out = self.torch.empty(c.B, c.T, c.D, dtype=self.torch.float32, device=self.device)
+            a = lc_entry_args(format=self.options.entry_format, rows=c.B * c.T, cols=c.D, y_dtype=LC_F32, y_ld=c.D)
+            lc_op_entry_unpack(a, ptr, None, out.data_ptr(), self.torch.cuda.current_stream(self.device).cuda_stream)
+            return out
         return self.arena[off:off + n].view(self.torch.float32).reshape(c.B, c.T, c.D).clone()
 
     def close(self):

@@ -22,6 +22,8 @@ using namespace lc;
 
 namespace lc {
 
+int check_sparse_args(const lc_sparse_args* a);  // lc_tokens.hip
+
 // y[r][:] = LN(x[r][:] (+ add[r][:])) * (1 + scale[:]) + shift[:], one wavefront per row; LN over D with biased
 // variance and no affine of its own. x, add fp32; y of type T. D % 4 == 0, D <= 64 * 4 * LN_MAXV.
 constexpr int LN_MAXV = 8;
@@ -125,14 +127,22 @@ inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 struct BlkW { void *wqkv, *wo, *w1, *w2; float *bqkv, *bo, *b1, *b2; };
 struct TPlan {
   int tc;  // rows of the token chunk, of the B*T of a step
-  size_t off_x, off_slots, slot_bytes, off_qkv, off_vt, off_ao, total;
+  size_t off_x, off_slots, slot_bytes, off_acc, off_qkv, off_vt, off_ao, off_means, off_index, off_part, part_bytes, total;
   int64_t step;  // rows of a pass of the MLP
 };
+// lc_dit_options with a rope table of its own
+struct TOpt {
+  lc_dit_options o;
+  lc_rope_table rope;
+  bool turns;
+};
+const TOpt kPlainOpt = {{LC_ENTRY_PLAIN, 0, 0, 0, 0, 0, nullptr, {0, 0, 0}}, {}, false};
 
 }  // namespace
 
 struct lc_dit {
   lc_dit_config cfg;
+  TOpt opt;
   hipStream_t cs, ss;
   int token_chunk;
   TPlan plan;
@@ -159,6 +169,11 @@ lc_status tfail(lc_dit* c, lc_status code, const char* fmt, ...) {
   if (c) c->err = buf; else g_terr = buf;
   return code;
 }
+#define LCT_OP(c, expr)                                                                           \
+  do {                                                                                            \
+    const lc_status s_ = (expr);                                                                  \
+    if (s_ != LC_OK) return tfail(c, s_, "%s", lc_last_error(nullptr));                           \
+  } while (0)
 #define LCT_HIP(c, expr)                                                                          \
   do {                                                                                            \
     hipError_t e_ = (expr);                                                                       \
@@ -192,12 +207,72 @@ inline size_t mlp_row_bytes(const lc_dit_config& g) {
   return (size_t)(1 + g.mlp_ratio) * g.D * dtype_size(g.dtype) + (gate_fused(g) ? 0 : (size_t)g.D * 4);
 }
 
-// Arena: the fp32 hidden states, dev_slots Delta entries (fp32), q,k,v + V^T + attention output of ALL tokens (a
+// the operators' descriptors for a step's q,k,v rows
+lc_rope_args rope_args(const lc_dit_config& g, const TOpt& t, int ldq) {
+  lc_rope_args a;
+  memset(&a, 0, sizeof a);
+  a.B = g.B; a.T = g.T; a.heads = 2 * g.heads; a.dtype = g.dtype;  // (the heads of k lie behind those of q)
+  a.x = a.y = lc_strides{(int64_t)g.T * ldq, ldq, g.head_dim};
+  for (int i = 0; i < 3; ++i) a.grid[i] = t.o.grid[i];
+  return a;
+}
+lc_sparse_args sparse_args(const lc_dit_config& g, const lc_dit_options& o) {
+  lc_sparse_args a;
+  memset(&a, 0, sizeof a);
+  a.B = g.B; a.Tq = a.Tk = g.T; a.heads = a.kv_heads = g.heads; a.head_dim = g.head_dim; a.dtype = g.dtype;
+  a.block = o.block; a.q_block = o.q_block; a.keep = o.keep; a.sink = o.sink; a.window = o.window;
+  a.q_prescaled = 1;
+  a.q = a.k = a.v = lc_strides{(int64_t)g.T * 3 * g.D, 3 * g.D, g.head_dim};
+  a.out = lc_strides{(int64_t)g.T * g.D, g.D, g.head_dim};
+  return a;
+}
+lc_entry_args entry_args(const lc_dit_config& g, const lc_dit_options& o) {
+  return lc_entry_args{o.entry_format, g.D, (int64_t)g.B * g.T, LC_F32, LC_F32, g.D, g.D};
+}
+inline size_t entry_bytes(const lc_dit_config& g, const TOpt& t) {
+  if (t.o.entry_format == LC_ENTRY_PLAIN) return (size_t)g.B * g.T * g.D * 4;
+  const lc_entry_args e = entry_args(g, t.o);
+  return lc_entry_packed_bytes(&e);
+}
+
+// opt (nullptr: none) -> *t
+lc_status check_topt(lc_dit* c, const lc_dit_config& g, const lc_dit_options* opt, TOpt* t) {
+  *t = kPlainOpt;
+  if (!opt) return LC_OK;
+  t->o = *opt;
+  t->o.rope = nullptr;
+  if (opt->entry_format < LC_ENTRY_PLAIN || opt->entry_format > LC_ENTRY_FP4) return tfail(c, LC_ERR_ARG, "entry_format must be one of LC_ENTRY_PLAIN .. LC_ENTRY_FP4");
+  if (opt->keep < 0) return tfail(c, LC_ERR_ARG, "keep must not be negative");
+  if (opt->keep > 0) {
+    const lc_sparse_args a = sparse_args(g, *opt);
+    const int s = check_sparse_args(&a);
+    if (s != LC_OK) return tfail(c, (lc_status)s, "%s", lc_last_error(nullptr));
+    if (opt->sink < 0) return tfail(c, LC_ERR_ARG, "sink must not be negative");
+    if ((int64_t)g.B * g.heads * lc_sparse_groups(&a) > (int64_t)1 << 22) return tfail(c, LC_ERR_SHAPE, "too many groups of queries");
+  }
+  if (opt->rope) {
+    t->rope = *opt->rope;
+    t->turns = true;
+    if (t->rope.checked != 1 || t->rope.axes < 1 || t->rope.axes > 3) return tfail(c, LC_ERR_ARG, "rope was not made by lc_rope_make");
+    if (t->rope.head_dim != g.head_dim) return tfail(c, LC_ERR_SHAPE, "rope is for heads of %d channels, the blocks have %d", t->rope.head_dim, g.head_dim);
+    if (g.B > 65535) return tfail(c, LC_ERR_SHAPE, "rope needs B of at most 65535");
+    int64_t cells = 1;
+    for (int i = 0; i < t->rope.axes; ++i) {
+      if (t->rope.axes > 1 && opt->grid[i] <= 0) return tfail(c, LC_ERR_SHAPE, "positions on several axes need a grid");
+      cells *= t->rope.axes > 1 ? opt->grid[i] : g.T;
+      if (cells > (int64_t)1 << 31) return tfail(c, LC_ERR_SHAPE, "the grid has more than 2^31 cells");
+    }
+    if (cells < g.T) return tfail(c, LC_ERR_SHAPE, "the grid has fewer cells than there are tokens");
+  }
+  return LC_OK;
+}
+
+// Arena: the fp32 hidden states, dev_slots Delta entries (fp32, or quantised, with one fp32 accumulator beside them), q,k,v + V^T + attention output of ALL tokens (a
 // query chunk attends to every key). The MLP runs when none of the latter is needed any more, and works there (see
 // run_block): with all tokens at once the arena is as much longer as a pass over all rows needs, with a token chunk by the
 // chunk's share of that. A pass then has room for the chunk in any case: what is held for all tokens covers at least its share
 // of the rest.
-TPlan make_tplan(const lc_dit_config& g, int token_chunk) {
+TPlan make_tplan(const lc_dit_config& g, int token_chunk, const TOpt& opt) {
   TPlan p;
   const size_t es = dtype_size(g.dtype);
   const int64_t R = (int64_t)g.B * g.T;
@@ -205,11 +280,23 @@ TPlan make_tplan(const lc_dit_config& g, int token_chunk) {
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes); return o; };
   p.off_x = take((size_t)R * g.D * 4);
-  p.slot_bytes = align_up((size_t)R * g.D * 4);
+  p.slot_bytes = align_up(entry_bytes(g, opt));
   p.off_slots = off; off += p.slot_bytes * g.dev_slots;
+  p.off_acc = off;
+  if (opt.o.entry_format != LC_ENTRY_PLAIN) take((size_t)R * g.D * 4);
   p.off_qkv = take((size_t)R * 3 * g.D * es);
-  p.off_vt = take((size_t)g.B * g.D * attn_tp(g.T) * es);
+  p.off_vt = off;
+  if (opt.o.keep == 0) take((size_t)g.B * g.D * attn_tp(g.T) * es);
   p.off_ao = take((size_t)R * g.D * es);
+  p.off_means = p.off_index = p.off_part = off;
+  p.part_bytes = 0;
+  if (opt.o.keep > 0) {  // the block means, the lists, and what workgroups that share a list hand over
+    const lc_sparse_args a = sparse_args(g, opt.o);
+    p.off_means = take((size_t)g.B * g.D * lc_sparse_blocks(&a) * sizeof(double));
+    p.off_index = take((size_t)g.B * g.heads * lc_sparse_groups(&a) * opt.o.keep * 4);
+    p.part_bytes = lc_block_attention_workspace(&a);
+    p.off_part = take(p.part_bytes);
+  }
   const size_t held = off - p.off_qkv, whole = (size_t)R * mlp_row_bytes(g);
   if (whole > held) take((size_t)(((unsigned __int128)(whole - held) * p.tc + R - 1) / R));
   p.total = off;
@@ -220,7 +307,6 @@ TPlan make_tplan(const lc_dit_config& g, int token_chunk) {
   return p;
 }
 
-inline size_t entry_bytes(const lc_dit_config& g) { return (size_t)g.B * g.T * g.D * 4; }
 inline char* slot_ptr(lc_dit* c, int s) { return c->arena + c->plan.off_slots + c->plan.slot_bytes * s; }
 // the six modulation vectors of every batch element for block blk: [B][6][D]
 inline const float* mod_blk(const lc_dit* c, const float* mod, int blk) { return mod + (int64_t)blk * c->cfg.B * 6 * c->cfg.D; }
@@ -291,7 +377,9 @@ lc_status run_block(lc_dit* c, int i, const float* mod, float* x, const float* d
   char* ao = c->arena + p.off_ao;
   lc_status s;
   const bool gated = gate_fused(g);
-  const bool vt_fused = g.dtype == kBF16 && lin2_covers(D, 3 * D) && 2 * D % (3 * D % 160 == 0 ? 160 : 128) == 0 && T % 4 == 0;
+  const TOpt& opt = c->opt;
+  const bool sparse = opt.o.keep > 0;
+  const bool vt_fused = !sparse && g.dtype == kBF16 && lin2_covers(D, 3 * D) && 2 * D % (3 * D % 160 == 0 ? 160 : 128) == 0 && T % 4 == 0;
   const int ldq = vt_fused ? 2 * D : 3 * D;
   // The chunk bounds the memory, and a pass takes as many rows as there is memory for: what is held for all tokens is not
   // needed all the time. The normalised rows of q,k,v lie where the attention output will be, the branch output (where it
@@ -302,8 +390,22 @@ lc_status run_block(lc_dit* c, int i, const float* mod, float* x, const float* d
   // ---- attention branch: q,k,v of every token first
   if ((s = ln_mod(c, x, delta, m, 0, 1, ao, (int)R, 0)) != LC_OK) return s;
   if ((s = linear(c, w.wqkv, w.bqkv, D, 3 * D, R, ao, qkv, 0, 0, D, vt_fused ? vt : nullptr)) != LC_OK) return s;
-  if (!vt_fused) LCT_HIP(c, launch_make_vt(c->cs, g.dtype, qkv + (size_t)2 * D * es, 3 * D, vt, g.B, T, Tp, D));
-  LCT_HIP(c, launch_spatial_attention(c->cs, g.dtype, qkv, ldq, vt, Tp, ao, g.B, T, g.heads, g.head_dim, 0, T, 1, g.B));
+  if (opt.turns) {  // (q carries the softmax scale already: a rotation does not mind)
+    const lc_rope_args a = rope_args(g, opt, ldq);
+    LCT_OP(c, lc_op_rope(&opt.rope, &a, qkv, nullptr, qkv, c->cs));
+  }
+  if (sparse) {
+    const lc_sparse_args a = sparse_args(g, opt.o);
+    double* const means = (double*)(c->arena + p.off_means);
+    int32_t* const index = (int32_t*)(c->arena + p.off_index);
+    const char *k = qkv + (size_t)D * es, *v = qkv + (size_t)2 * D * es;
+    LCT_OP(c, lc_op_block_means(&a, k, nullptr, means, 0, lc_sparse_blocks(&a), c->cs));
+    LCT_OP(c, lc_op_block_select(&a, qkv, means, nullptr, nullptr, index, c->cs));
+    LCT_OP(c, lc_op_block_attention(&a, qkv, k, v, index, nullptr, nullptr, ao, c->arena + p.off_part, p.part_bytes, c->cs));
+  } else {
+    if (!vt_fused) LCT_HIP(c, launch_make_vt(c->cs, g.dtype, qkv + (size_t)2 * D * es, 3 * D, vt, g.B, T, Tp, D));
+    LCT_HIP(c, launch_spatial_attention(c->cs, g.dtype, qkv, ldq, vt, Tp, ao, g.B, T, g.heads, g.head_dim, 0, T, 1, g.B));
+  }
   if (gated) {
     if ((s = linear_gated(c, w.wo, w.bo, D, R, ao, dst, m, 2, 0)) != LC_OK) return s;
   } else {
@@ -342,7 +444,9 @@ lc_status run_step(lc_dit* c, const void* x_in, const void* mod, void* x_out, in
   const lc_dit_config& g = c->cfg;
   const int64_t R = (int64_t)g.B * g.T;
   float* x = (float*)(c->arena + c->plan.off_x);
-  float* delta = (float*)slot_ptr(c, slot);
+  const bool packed = c->opt.o.entry_format != LC_ENTRY_PLAIN;
+  const lc_entry_args entry = entry_args(g, c->opt.o);
+  float* delta = packed ? (float*)(c->arena + c->plan.off_acc) : (float*)slot_ptr(c, slot);
   const float* m = (const float*)mod;
   LCT_HIP(c, hipMemcpyAsync(x, x_in, (size_t)R * g.D * 4, hipMemcpyDeviceToDevice, c->cs));
   lc_status s;
@@ -356,13 +460,18 @@ lc_status run_step(lc_dit* c, const void* x_in, const void* mod, void* x_out, in
     LCT_HIP(c, launch_fill_f32(c->cs, delta, R * g.D, 0.f));
     for (int i = g.cache_a; i < g.cache_b; ++i)
       if ((s = run_block(c, i, m, x, delta, delta)) != LC_OK) return s;
+    if (packed) LCT_OP(c, lc_op_entry_pack(&entry, delta, slot_ptr(c, slot), x, x, c->cs));  // (x_b = x_a + what the entry stands for)
     LCT_HIP(c, hipEventRecord(c->ev_produced[slot], c->cs));
     c->dev_filled[slot] = 1;
   } else if (c->in_pending[slot]) {
     LCT_HIP(c, hipStreamWaitEvent(c->cs, c->ev_in_done[slot], 0));
     c->in_pending[slot] = 0;
   }
-  if ((s = gate_add(c, x, delta, nullptr, 0, R, 0)) != LC_OK) return s;  // x_b = x_a + Delta, at both kinds of step
+  if (!packed) {
+    if ((s = gate_add(c, x, delta, nullptr, 0, R, 0)) != LC_OK) return s;  // x_b = x_a + Delta, at both kinds of step
+  } else if (!full) {
+    LCT_OP(c, lc_op_entry_unpack(&entry, slot_ptr(c, slot), x, x, c->cs));
+  }
   LCT_HIP(c, hipEventRecord(c->ev_consumed[slot], c->cs));
   for (int i = g.cache_b; i < g.L; ++i)
     if ((s = run_block(c, i, m, x, nullptr, x)) != LC_OK) return s;
@@ -385,11 +494,25 @@ extern "C" {
 
 const char* lc_dit_last_error(const lc_dit* c) { return c ? c->err.c_str() : g_terr.c_str(); }
 lc_status lc_dit_check_config(const lc_dit_config* cfg) { return check_tcfg(nullptr, cfg); }
-size_t lc_dit_entry_bytes(const lc_dit_config* cfg) { return check_tcfg(nullptr, cfg) == LC_OK ? entry_bytes(*cfg) : 0; }
-size_t lc_dit_workspace_bytes(const lc_dit_config* cfg, int token_chunk) {
-  if (check_tcfg(nullptr, cfg) != LC_OK) return 0;
+size_t lc_dit_entry_bytes(const lc_dit_config* cfg) { return lc_dit_options_entry_bytes(cfg, nullptr); }
+size_t lc_dit_workspace_bytes(const lc_dit_config* cfg, int token_chunk) { return lc_dit_options_workspace_bytes(cfg, nullptr, token_chunk); }
+lc_status lc_dit_check_options(const lc_dit_config* cfg, const lc_dit_options* opt) {
+  const lc_status s = check_tcfg(nullptr, cfg);
+  if (s != LC_OK) return s;
+  if (!opt) return tfail(nullptr, LC_ERR_ARG, "opt is NULL");
+  TOpt t;
+  return check_topt(nullptr, *cfg, opt, &t);
+}
+size_t lc_dit_options_entry_bytes(const lc_dit_config* cfg, const lc_dit_options* opt) {
+  TOpt t;
+  if (check_tcfg(nullptr, cfg) != LC_OK || check_topt(nullptr, *cfg, opt, &t) != LC_OK) return 0;
+  return entry_bytes(*cfg, t);
+}
+size_t lc_dit_options_workspace_bytes(const lc_dit_config* cfg, const lc_dit_options* opt, int token_chunk) {
+  TOpt t;
+  if (check_tcfg(nullptr, cfg) != LC_OK || check_topt(nullptr, *cfg, opt, &t) != LC_OK) return 0;
   if (token_chunk < 0) { g_terr = "token_chunk must be >= 0"; return 0; }
-  return make_tplan(*cfg, token_chunk).total;
+  return make_tplan(*cfg, token_chunk, t).total;
 }
 
 lc_status lc_dit_destroy(lc_dit* c) {
@@ -415,12 +538,13 @@ lc_status lc_dit_create(const lc_dit_config* cfg, void* compute_stream, void* si
   c->cfg = *cfg;
   c->cs = (hipStream_t)compute_stream; c->ss = (hipStream_t)side_stream;
   c->token_chunk = 0;
-  c->plan = make_tplan(c->cfg, 0);
+  c->opt = kPlainOpt;
+  c->plan = make_tplan(c->cfg, 0, c->opt);
   c->arena = nullptr; c->arena_bytes = 0; c->have_weights = false; c->wblob = nullptr;
   c->full_steps = c->cached_steps = c->swaps_out = c->swaps_in = 0;
   for (int i = 0; i < cfg->host_slots; ++i) {
     void* p = nullptr;
-    if (hipHostMalloc(&p, entry_bytes(*cfg), hipHostMallocDefault) != hipSuccess) {
+    if (hipHostMalloc(&p, entry_bytes(*cfg, c->opt), hipHostMallocDefault) != hipSuccess) {
       (void)hipGetLastError();
       lc_dit_destroy(c);
       return tfail(nullptr, LC_ERR_NOMEM, "hipHostMalloc (pinned cache bank) failed");
@@ -498,10 +622,42 @@ lc_status lc_dit_set_workspace(lc_dit* c, void* arena, size_t bytes) {
 lc_status lc_dit_set_chunk(lc_dit* c, int token_chunk) {
   if (!c) return tfail(nullptr, LC_ERR_ARG, "ctx is NULL");
   if (token_chunk < 0) return tfail(c, LC_ERR_ARG, "token_chunk must be >= 0");
-  TPlan np = make_tplan(c->cfg, token_chunk);
+  TPlan np = make_tplan(c->cfg, token_chunk, c->opt);
   if (c->arena && np.total > c->arena_bytes) return tfail(c, LC_ERR_NOMEM, "chunk setting needs %zu bytes, workspace has %zu", np.total, c->arena_bytes);
   c->token_chunk = token_chunk;  // (the hidden states and the slots sit at chunk-independent offsets)
   c->plan = np;
+  return LC_OK;
+}
+
+lc_status lc_dit_set_options(lc_dit* c, const lc_dit_options* opt) {
+  if (!c) return tfail(nullptr, LC_ERR_ARG, "ctx is NULL");
+  TOpt t;
+  const lc_status s = check_topt(c, c->cfg, opt, &t);
+  if (s != LC_OK) return s;
+  const TPlan np = make_tplan(c->cfg, c->token_chunk, t);
+  if (c->arena && np.total > c->arena_bytes) return tfail(c, LC_ERR_NOMEM, "the options need %zu bytes, workspace has %zu", np.total, c->arena_bytes);
+  LCT_HIP(c, hipStreamSynchronize(c->cs));
+  LCT_HIP(c, hipStreamSynchronize(c->ss));
+  if (entry_bytes(c->cfg, t) != entry_bytes(c->cfg, c->opt)) {
+    void* bank[64];  // (host_slots is at most that)
+    size_t n = 0;
+    for (; n < c->host.size(); ++n) {
+      if (hipHostMalloc(&bank[n], entry_bytes(c->cfg, t), hipHostMallocDefault) != hipSuccess) {
+        (void)hipGetLastError();
+        while (n > 0) (void)hipHostFree(bank[--n]);
+        return tfail(c, LC_ERR_NOMEM, "hipHostMalloc (pinned cache bank) failed");
+      }
+    }
+    for (size_t i = 0; i < n; ++i) {
+      (void)hipHostFree(c->host[i]);
+      c->host[i] = bank[i];
+    }
+  }
+  c->opt = t;
+  c->plan = np;
+  std::fill(c->host_filled.begin(), c->host_filled.end(), 0);
+  std::fill(c->dev_filled.begin(), c->dev_filled.end(), 0);
+  std::fill(c->in_pending.begin(), c->in_pending.end(), 0);
   return LC_OK;
 }
 
@@ -535,7 +691,7 @@ lc_status lc_dit_swap_out(lc_dit* c, int dev_slot, int host_slot) {
   if (s != LC_OK) return s;
   if (!c->dev_filled[dev_slot]) return tfail(c, LC_ERR_STATE, "swap-out of empty device slot %d", dev_slot);
   LCT_HIP(c, hipStreamWaitEvent(c->ss, c->ev_produced[dev_slot], 0));
-  LCT_HIP(c, hipMemcpyAsync(c->host[host_slot], slot_ptr(c, dev_slot), entry_bytes(c->cfg), hipMemcpyDeviceToHost, c->ss));
+  LCT_HIP(c, hipMemcpyAsync(c->host[host_slot], slot_ptr(c, dev_slot), entry_bytes(c->cfg, c->opt), hipMemcpyDeviceToHost, c->ss));
   LCT_HIP(c, hipEventRecord(c->ev_rd_done[dev_slot], c->ss));
   c->host_filled[host_slot] = 1;
   c->swaps_out++;
@@ -548,7 +704,7 @@ lc_status lc_dit_swap_in(lc_dit* c, int host_slot, int dev_slot) {
   if (!c->host_filled[host_slot]) return tfail(c, LC_ERR_STATE, "swap-in from empty host slot %d", host_slot);
   LCT_HIP(c, hipStreamWaitEvent(c->ss, c->ev_consumed[dev_slot], 0));
   LCT_HIP(c, hipStreamWaitEvent(c->ss, c->ev_produced[dev_slot], 0));
-  LCT_HIP(c, hipMemcpyAsync(slot_ptr(c, dev_slot), c->host[host_slot], entry_bytes(c->cfg), hipMemcpyHostToDevice, c->ss));
+  LCT_HIP(c, hipMemcpyAsync(slot_ptr(c, dev_slot), c->host[host_slot], entry_bytes(c->cfg, c->opt), hipMemcpyHostToDevice, c->ss));
   LCT_HIP(c, hipEventRecord(c->ev_in_done[dev_slot], c->ss));
   c->in_pending[dev_slot] = 1;
   c->dev_filled[dev_slot] = 1;
@@ -571,7 +727,12 @@ lc_status lc_dit_cache_write(lc_dit* c, int dev_slot, const void* delta) {
   LCT_HIP(c, hipStreamWaitEvent(c->cs, c->ev_rd_done[dev_slot], 0));
   LCT_HIP(c, hipStreamWaitEvent(c->cs, c->ev_in_done[dev_slot], 0));
   c->in_pending[dev_slot] = 0;
-  LCT_HIP(c, hipMemcpyAsync(slot_ptr(c, dev_slot), delta, entry_bytes(c->cfg), hipMemcpyDeviceToDevice, c->cs));
+  if (c->opt.o.entry_format != LC_ENTRY_PLAIN) {
+    const lc_entry_args entry = entry_args(c->cfg, c->opt.o);
+    LCT_OP(c, lc_op_entry_pack(&entry, delta, slot_ptr(c, dev_slot), nullptr, nullptr, c->cs));
+  } else {
+    LCT_HIP(c, hipMemcpyAsync(slot_ptr(c, dev_slot), delta, entry_bytes(c->cfg, c->opt), hipMemcpyDeviceToDevice, c->cs));
+  }
   LCT_HIP(c, hipEventRecord(c->ev_produced[dev_slot], c->cs));
   c->dev_filled[dev_slot] = 1;
   return LC_OK;
@@ -583,7 +744,7 @@ lc_status lc_dit_cache_peek(lc_dit* c, int host_slot, const void** ptr, size_t* 
   if (host_slot < 0 || host_slot >= c->cfg.host_slots) return tfail(c, LC_ERR_ARG, "host slot %d out of range", host_slot);
   if (!c->host_filled[host_slot]) return tfail(c, LC_ERR_STATE, "host slot %d is empty", host_slot);
   *ptr = c->host[host_slot];
-  *bytes = entry_bytes(c->cfg);
+  *bytes = entry_bytes(c->cfg, c->opt);
   return LC_OK;
 }
 
@@ -594,7 +755,7 @@ lc_status lc_dit_cache_dev_peek(lc_dit* c, int dev_slot, const void** ptr, size_
   if (!c->arena) return tfail(c, LC_ERR_STATE, "workspace not set");
   if (!c->dev_filled[dev_slot]) return tfail(c, LC_ERR_STATE, "device slot %d is empty", dev_slot);
   *ptr = slot_ptr(c, dev_slot);
-  *bytes = entry_bytes(c->cfg);
+  *bytes = entry_bytes(c->cfg, c->opt);
   return LC_OK;
 }
 
