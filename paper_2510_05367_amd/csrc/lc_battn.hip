@@ -19,7 +19,6 @@ int check_sparse_rows(const char* name, const void* p, const lc_strides& s, int 
 
 namespace {
 
-constexpr int kRawBuffer = 0x00020000;  // resource word 3: raw 32-bit data
 typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
@@ -29,10 +28,13 @@ struct BlockAttnArgs {
   float* part;      // several workgroups a list: [query of all][split][D] sums, then [query of all][split][2] maxima and denominators
   float scale;      // of a score, to log2 units
   int B, Tq, Tk, H, Hkv, block, q_block, keep, nq, splits;
+  int unit;         // heads in a row that go to one XCD (0: workgroups are dealt out as they come)
 };
 
 // KS: wavefronts that share a tile of 32 queries and take turns at its keys. 1: four tiles (groups of up to 128 queries), every
-// wavefront takes both halves of a chunk; 2: two tiles, a half each; 4: one tile, and two chunks at a time.
+// wavefront takes all keys; 2: two tiles, 32 of the 64 keys of a chunk each; 4: one tile, and two chunks at a time. (Two tiles a
+// wavefront halve the fragment reads, but leave room for two wavefronts a SIMD in place of four: 16 heads of 64, 16 of 64 blocks,
+// 2 x 4096 tokens 51 and 56 us, groups of 64 queries 56 and 69; LDS is not what bounds this.)
 template <class T, int D, int KS> struct BlockAttnShape {
   static constexpr int VEC = Vec16<T>::N;
   static constexpr int PK = D / VEC;             // 16-byte packets of a row
@@ -41,8 +43,9 @@ template <class T, int D, int KS> struct BlockAttnShape {
   static constexpr int TILE = 64 * KP * 16;      // bytes of a chunk's K rows, or of its V rows
   static constexpr int NCH = KS == 4 && 2 * TILE <= 32768 ? 2 : 1;  // chunks of a stage
   static constexpr int STAGE = NCH * 2 * TILE;
-  static constexpr int NB = STAGE <= 16384 ? 4 : 2;                 // stages in LDS
-  static constexpr int RED = KS == 1 ? 0 : 4 * (DM * 32 * 33 + 64) * 4;  // what wavefronts hand over at the end
+  static constexpr int NB = 2;                   // stages in LDS
+  static constexpr int HAND = (DM * 16 + 2) * 64 * 4;  // what a wavefront hands to another at the end
+  static constexpr int RED = KS == 1 ? 0 : 2 * HAND;
   static constexpr int LDS = NB * STAGE > RED ? NB * STAGE : RED;
   static constexpr int LPW = NCH * KP / 2;       // loads of a stage that a wavefront issues
 };
@@ -56,21 +59,21 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
   constexpr int KT = KS == 1 ? 2 : 1;      // 32-key sub-tiles of a stage and wavefront
   constexpr int STEPS = KP / 2;            // packets a lane contracts along d
   constexpr bool BF = sizeof(T) == 2;
+  constexpr bool kPrio = BF && D <= 64;
   constexpr bool POW2 = (KP & (KP - 1)) == 0;
-  constexpr int PD = NB - 1;               // stages in flight
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  int* const n_list = reinterpret_cast<int*>(smem);  // (before the first stage lands there)
 
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, hh = lane >> 5;
-  // all groups of a (batch element, head) on one XCD, whose L2 then fetches its keys and values once
+  // Workgroups are handed to the XCDs in turn: all that read the same keys and values (the groups of a head, and the heads that
+  // share it) are put on one, whose L2 then fetches them once
   int prob, in;
   {
-    const int per = a.nq * a.splits, nprob = a.B * a.H, id = blockIdx.x;
-    if (nprob % 8 == 0) {
-      const int slot = id >> 3, p8 = slot / per;
-      prob = (id & 7) + 8 * p8;
-      in = slot - p8 * per;
+    const int per = a.nq * a.splits, run = a.unit * per, id = blockIdx.x;
+    if (a.unit > 0) {
+      const int slot = id >> 3, u8 = slot / run, w = slot - u8 * run, p = w / per;
+      prob = ((id & 7) + 8 * u8) * a.unit + p;
+      in = w - p * per;
     } else {
       prob = id / per;
       in = id - prob * per;
@@ -81,10 +84,10 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
   const int row0 = g * a.q_block, rows = min(min(a.q_len ? max(a.q_len[b], 0) : a.Tq, a.Tq) - row0, a.q_block);
   if (rows <= 0) return;
   const int32_t* const list = a.index + ((int64_t)prob * a.nq + g) * a.keep;
+  int ent = list[min(lane, a.keep - 1)];  // a lane holds an entry of the list, 64 at a time
 
   // ---- queries: B operand of S^T = K Q^T; packets beyond D and rows beyond the group are zeros
-  const int tile = KS == 1 ? wid : KS == 2 ? wid >> 1 : 0;
-  const int qi = tile * 32 + lq;
+  const int qi = wid / KS * 32 + lq;
   Vec16<T> qf[STEPS];
 #pragma unroll
   for (int j = 0; j < STEPS; ++j) {
@@ -93,18 +96,21 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
   }
 
   // the list ends before its first entry that is no existing block or does not ascend
-  if (tid == 0) *n_list = a.keep;
-  __syncthreads();
-  for (int i = tid; i < a.keep; i += 256) {
-    const int e = list[i];
-    if (e < 0 || (int64_t)e * a.block >= TK || (i > 0 && e <= list[i - 1])) atomicMin(n_list, i);
+  int n = a.keep;
+  for (int i0 = 0, last = -1; i0 < a.keep; i0 += 64) {
+    const int e = i0 == 0 ? ent : list[min(i0 + lane, a.keep - 1)];
+    const int prev = __shfl_up(e, 1, 64);
+    const bool bad = i0 + lane < a.keep && (e < 0 || (int64_t)e * a.block >= TK || e <= (lane == 0 ? last : prev));
+    const uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
+    if (bads != 0) {
+      n = i0 + __builtin_ctzll(bads);
+      break;
+    }
+    last = __builtin_amdgcn_readlane(e, 63);
   }
-  __syncthreads();
-  const int cpb = a.block / 64;
-  const int chunks = __builtin_amdgcn_readfirstlane(*n_list) * cpb;
+  const int cpb = a.block / 64, chunks = __builtin_amdgcn_readfirstlane(n) * cpb;
   const int c_lo = (int)((int64_t)chunks * split / a.splits), c_hi = (int)((int64_t)chunks * (split + 1) / a.splits);
   const int nstage = (c_hi - c_lo + NCH - 1) / NCH;
-  __syncthreads();
 
   // ---- what this wavefront moves: K or V rows of one chunk of a stage, or half of them
   const int my_chunk = NCH == 2 ? wid >> 1 : 0;
@@ -126,13 +132,8 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
     off[i] = c < PK ? (uint32_t)(key * ld + c * VEC) * (uint32_t)sizeof(T) : 0x7fffff00u;
   }
   const unsigned lds_at = (my_chunk * 2 + (moves_v ? 1 : 0)) * S::TILE + first * 1024;
-  // The chunks of the list in turn, TK (no keys) behind the end: a lane holds an entry, 64 at a time
-  int at = c_lo + my_chunk, at_li = at / cpb, at_sub = at - at_li * cpb, held = at_li & ~63;
-  int ent = list[min(held + lane, a.keep - 1)];
-  // (everything loaded so far is waited for here, not where the loop uses it: the requests below must stay in flight)
-  asm volatile("" : "+v"(ent));
-#pragma unroll
-  for (int j = 0; j < STEPS; ++j) asm volatile("" : "+v"(qf[j].v));
+  // The chunks of the list in turn, TK (no keys) behind the end
+  int at = c_lo + my_chunk, at_li = at / cpb, at_sub = at - at_li * cpb, held = 0;
   auto next_key0 = [&]() {
     if (at >= c_hi) return TK;
     if (at_li - held >= 64) {
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
     const uint64_t base = (uint64_t)(src + key0 * ld);
     typedef __attribute__((ext_vector_type(4))) int i32x4;
     const i32x4 r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xffffu)),
-                     __builtin_amdgcn_readfirstlane(keys > 0 ? (int)(((keys - 1) * ld + D) * (int)sizeof(T)) : 0), kRawBuffer};
+                     __builtin_amdgcn_readfirstlane(keys > 0 ? (int)(((keys - 1) * ld + D) * (int)sizeof(T)) : 0), 0x00020000};  // (raw 32-bit data)
     const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)(smem + (st % NB) * S::STAGE + lds_at));
     asm volatile("s_nop 4" ::: "memory");
 #pragma unroll
@@ -192,21 +193,22 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[mt][r] = 0.f;
 
-  int k0[PD + 1];  // first keys of the stages in flight
+  // (what the loop uses of earlier loads is waited for in front of it: there the requests must stay in flight)
+  asm volatile("" : "+v"(ent));
+  int now = next_key0();
+  if (nstage > 0) issue(0, now);
 #pragma unroll
-  for (int s = 0; s < PD; ++s) {
-    k0[s] = next_key0();
-    issue(s, k0[s]);
-  }
+  for (int j = 0; j < STEPS; ++j) asm volatile("" : "+v"(qf[j].v));
   for (int st = 0; st < nstage; ++st) {
-    // stage st has landed for everyone, and nobody still reads the buffer that the next request goes to. (Behind the last stage the
-    // requests deliver zeros: their number stays what the wait counts on.)
-    barrier_keep<(PD - 1) * LPW>();
-    k0[PD] = next_key0();
-    issue(st + PD, k0[PD]);
+    barrier_keep<0>();  // stage st has landed for everyone, and nobody still reads the other buffer
+    const int next = next_key0();
+    if (st + 1 < nstage) issue(st + 1, next);
     const unsigned char* const buf = smem + (st % NB) * S::STAGE;
-    const int key0 = k0[0] + half * 32;
+    const int key0 = now + half * 32;
     if (busy && key0 < TK) {
+      // (matrix phases go first where wavefronts compete: 609 -> 598 us at 33001 tokens, 64 of 516 blocks; with 128 channels, where there
+      // are two wavefronts a SIMD, 43 -> 44 at 2 x 4096)
+      if (kPrio) __builtin_amdgcn_s_setprio(1);
       f32x16 sc[KT];
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
@@ -223,8 +225,9 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
           }
         }
       }
+      if (kPrio) __builtin_amdgcn_s_setprio(0);
       // lane holds keys key0 + 32 kt + 8 (r / 4) + 4 hh + r % 4 of query lq
-      if (k0[0] + 64 > TK) {
+      if (now + 64 > TK) {
         int kb = key0 + 4 * hh;
         asm volatile("" : "+v"(kb));  // (left alone the compiler computes the indexes outside the branch)
 #pragma unroll
@@ -271,6 +274,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
             l = __builtin_amdgcn_fdot2_f32_bf16(p2, one2, l, false);
 #endif
           }
+          if (kPrio) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
           for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -278,9 +282,9 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
               bf16x8 vf = {};
 #ifdef __HIP_DEVICE_COMPILE__
               typedef __attribute__((address_space(3))) s16x4* tr_ptr;
-              const unsigned char* const at = buf + v_at + v_off[mt] + ((half + kt) * 32 + 16 * s) * (KP * 16);
-              const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at));
-              const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 8 * (KP * 16)));
+              const unsigned char* const p = buf + v_at + v_off[mt] + ((half + kt) * 32 + 16 * s) * (KP * 16);
+              const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p));
+              const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(p + 8 * (KP * 16)));
               const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
               vf = __builtin_bit_cast(bf16x8, both);
 #else
@@ -288,6 +292,7 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
 #endif
               M::mma(vf, pf[s], o[mt]);
             }
+          if (kPrio) __builtin_amdgcn_s_setprio(0);
         } else {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -302,106 +307,73 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
         }
       }
     }
-#pragma unroll
-    for (int s = 0; s < PD; ++s) k0[s] = k0[s + 1];
+    now = next;
   }
-  // (a wavefront must not end, nor the stages be used for anything else, with requests for them under way)
-  __builtin_amdgcn_s_waitcnt(waitcnt_imm(0));
-  l += __shfl_xor(l, 32, 64);
 
-  T* const ob = out + b * a.os.batch + h * a.os.head;
-  const int64_t pq = (int64_t)prob * a.Tq + row0;  // this group's first query, counted over all
-  float* const pml = a.part + (int64_t)a.B * a.H * a.Tq * a.splits * D;
-  if constexpr (KS == 1) {
-    if (qi >= rows) return;
-    if (a.splits > 1) {
-      float* const po = a.part + ((pq + qi) * a.splits + split) * D;
+  // ---- wavefronts that shared queries: every second one hands its sums to the one before, which brings both to the larger of
+  // their offsets and adds them; then the third to the first (a fixed order)
+  if constexpr (KS > 1) {
 #pragma unroll
-      for (int mt = 0; mt < DM; ++mt)
+    for (int step = 1; step < KS; step *= 2) {
+      const bool gives = (wid & (2 * step - 1)) == step, takes = (wid & (2 * step - 1)) == 0;
+      float* const box = reinterpret_cast<float*>(smem + (step == 1 ? wid >> 1 : 0) * S::HAND) + lane;
+      __syncthreads();
+      if (gives) {
+        box[0] = m;
+        box[64] = l;
 #pragma unroll
-        for (int gr = 0; gr < 4; ++gr) {
-          const int dim = mt * 32 + 8 * gr + 4 * hh;
-          if (dim < D) *reinterpret_cast<f32x4*>(po + dim) = f32x4{o[mt][4 * gr], o[mt][4 * gr + 1], o[mt][4 * gr + 2], o[mt][4 * gr + 3]};
-        }
-      if (hh == 0) {
-        float* const w = pml + ((pq + qi) * a.splits + split) * 2;
-        w[0] = m;
-        w[1] = l;
+        for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) box[(2 + mt * 16 + r) * 64] = o[mt][r];
       }
-      return;
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* const orow = ob + (int64_t)(row0 + qi) * a.os.token;
+      __syncthreads();
+      if (takes) {
+        const float mo = box[0], top = fmaxf(m, mo);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), fo = mo == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mo - top);
+        m = top;
+        l = l * f + box[64] * fo;
 #pragma unroll
-    for (int mt = 0; mt < DM; ++mt)
+        for (int mt = 0; mt < DM; ++mt)
 #pragma unroll
-      for (int gr = 0; gr < 4; ++gr) {
-        const int dim = mt * 32 + 8 * gr + 4 * hh;
-        if (dim < D) {
-          if constexpr (BF) {
-            bf16x4 ov;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) ov[e] = static_cast<bf16_t>(o[mt][4 * gr + e] * inv);
-            *reinterpret_cast<bf16x4*>(orow + dim) = ov;
-          } else {
-            *reinterpret_cast<f32x4*>(orow + dim) = f32x4{o[mt][4 * gr] * inv, o[mt][4 * gr + 1] * inv, o[mt][4 * gr + 2] * inv, o[mt][4 * gr + 3] * inv};
-          }
-        }
-      }
-  } else {
-    // ---- the wavefronts of a tile bring their sums to the largest of their offsets and add them, in a fixed order
-    barrier_keep<0>();
-    float* const red = reinterpret_cast<float*>(smem);  // [wavefront][dim][33]: O^T of the 32 queries
-    float* const ml = red + 4 * DM * 32 * 33;            // [wavefront][offset | denominator][32]
-    if (hh == 0) {
-      ml[wid * 64 + lq] = m;
-      ml[wid * 64 + 32 + lq] = l;
-    }
-    __syncthreads();
-    auto factor = [](float mw, float top) { return mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top); };
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < KS; ++w) top = fmaxf(top, ml[(tile * KS + w) * 64 + lq]);
-    const float f = factor(m, top);
-#pragma unroll
-    for (int mt = 0; mt < DM; ++mt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) red[((wid * DM + mt) * 32 + 8 * (r >> 2) + 4 * hh + (r & 3)) * 33 + lq] = o[mt][r] * f;
-    __syncthreads();
-    constexpr int QN = 128 / KS, TPQ = 256 / QN, ND = DM * 32 / TPQ;  // queries; threads a query; dims a thread
-    const int tq = tid / TPQ, td = tid % TPQ * ND, w0 = tq / 32 * KS, ql = tq & 31;
-    if (tq >= rows) return;
-    float lt = 0.f, mt_ = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < KS; ++w) mt_ = fmaxf(mt_, ml[(w0 + w) * 64 + ql]);
-#pragma unroll
-    for (int w = 0; w < KS; ++w) lt += ml[(w0 + w) * 64 + 32 + ql] * factor(ml[(w0 + w) * 64 + ql], mt_);
-    const bool whole = a.splits == 1;
-    const float inv = !whole ? 1.f : lt == 0.f ? 0.f : 1.f / lt;
-    T* const orow = ob + (int64_t)(row0 + tq) * a.os.token;
-    float* const po = a.part + ((pq + tq) * a.splits + split) * D;
-#pragma unroll
-    for (int e = 0; e < ND; e += 4) {
-      if (td + e < D) {
-        float s[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[i] = 0.f;
-#pragma unroll
-          for (int w = 0; w < KS; ++w) s[i] += red[((w0 + w) * DM * 32 + td + e + i) * 33 + ql];
-        }
-        if (!whole) *reinterpret_cast<f32x4*>(po + td + e) = f32x4{s[0], s[1], s[2], s[3]};
-        else
-#pragma unroll
-          for (int i = 0; i < 4; ++i) orow[td + e + i] = from_f32<T>(s[i] * inv);
+          for (int r = 0; r < 16; ++r) o[mt][r] = o[mt][r] * f + box[(2 + mt * 16 + r) * 64] * fo;
       }
     }
-    if (!whole && td == 0) {
-      float* const w = pml + ((pq + tq) * a.splits + split) * 2;
-      w[0] = mt_;
-      w[1] = lt;
-    }
+    if (wid % KS != 0) return;
   }
+
+  // ---- lane holds O^T[dim = 32 mt + 8 (r / 4) + 4 hh + r % 4][query lq]
+  l += __shfl_xor(l, 32, 64);
+  if (qi >= rows) return;
+  const int64_t pq = (int64_t)prob * a.Tq + row0 + qi;  // this query, counted over all
+  const float inv = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+  float* const po = a.part + (pq * a.splits + split) * D;
+  T* const orow = out + b * a.os.batch + h * a.os.head + (int64_t)(row0 + qi) * a.os.token;
+  if (a.splits > 1 && hh == 0) {
+    float* const w = a.part + (int64_t)a.B * a.H * a.Tq * a.splits * D + (pq * a.splits + split) * 2;
+    w[0] = m;
+    w[1] = l;
+  }
+#pragma unroll
+  for (int mt = 0; mt < DM; ++mt)
+#pragma unroll
+    for (int gr = 0; gr < 4; ++gr) {
+      const int dim = mt * 32 + 8 * gr + 4 * hh;
+      if (dim < D) {
+        f32x4 ov;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ov[e] = o[mt][4 * gr + e] * inv;
+        if (a.splits > 1) {
+          *reinterpret_cast<f32x4*>(po + dim) = ov;
+        } else if constexpr (BF) {
+          bf16x4 ob;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ob[e] = static_cast<bf16_t>(ov[e]);
+          *reinterpret_cast<bf16x4*>(orow + dim) = ob;
+        } else {
+          *reinterpret_cast<f32x4*>(orow + dim) = ov;
+        }
+      }
+    }
 }
 
 // out = the splits' sums brought to one offset, added in a fixed order and divided; a thread four dims of a query
@@ -479,10 +451,10 @@ template <class T, int D, int KS> hipError_t run_block_attn(hipStream_t s, const
   return hipGetLastError();
 }
 template <class T> hipError_t block_attn_dispatch(hipStream_t s, const BlockAttnArgs& a, int d, int ks, const void* q, const void* k, const void* v, void* out) {
-#define LC_GO(D)                                              \
-  case D:                                                     \
-    return ks == 1 ? run_block_attn<T, D, 1>(s, a, q, k, v, out) \
-         : ks == 2 ? run_block_attn<T, D, 2>(s, a, q, k, v, out) \
+#define LC_GO(D)                                                   \
+  case D:                                                          \
+    return ks == 1 ? run_block_attn<T, D, 1>(s, a, q, k, v, out)   \
+         : ks == 2 ? run_block_attn<T, D, 2>(s, a, q, k, v, out)   \
                    : run_block_attn<T, D, 4>(s, a, q, k, v, out)
   switch (d) {
     LC_GO(8);
@@ -530,6 +502,8 @@ lc_status lc_op_block_attention(const lc_sparse_args* a, const void* q, const vo
   k_.scale = a->q_prescaled ? 1.f : attn_q_scale(a->head_dim);
   k_.B = a->B; k_.Tq = a->Tq; k_.Tk = a->Tk; k_.H = a->heads; k_.Hkv = a->kv_heads; k_.block = a->block; k_.q_block = a->q_block;
   k_.keep = a->keep; k_.nq = lc_sparse_groups(a); k_.splits = list_splits(a);
+  const int64_t kvs = (int64_t)a->B * a->kv_heads;
+  k_.unit = kvs % 8 == 0 ? a->heads / a->kv_heads : kvs * (a->heads / a->kv_heads) % 8 == 0 ? 1 : 0;
   const int ks = tiles_shared(a);
   hipError_t e = a->dtype == LC_BF16 ? block_attn_dispatch<bf16_t>((hipStream_t)stream, k_, a->head_dim, ks, q, k, v, out)
                                      : block_attn_dispatch<float>((hipStream_t)stream, k_, a->head_dim, ks, q, k, v, out);
