@@ -1,6 +1,7 @@
 // Operators over the tokens of long videos: rotary positions, block means, selection of key blocks.
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "../../include/lightcache.h"
 #include "lc_internal.h"
@@ -120,8 +121,27 @@ inline bool strides_aligned(const void* p, const lc_strides& s, int dt, size_t b
 
 // ---- block means -----------------------------------------------------------------------------------------------------
 
+// acc += rows r0, r0 + step, .. < n of a packet of channels, eight of them under way at a time (the sums are nothing to the loads). In 64 bits:
+// those of bf16 are then exact.
+template <class T>
+__device__ __forceinline__ void sum_rows(const T* base, int64_t ld, int r0, int step, int n, double (&acc)[Vec16<T>::N]) {
+  constexpr int AHEAD = 8;
+  for (int r = r0; r < n; r += AHEAD * step) {
+    Vec16<T> v[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) v[u] = load16(base + (int64_t)min(r + u * step, n - 1) * ld);
+    __builtin_amdgcn_sched_barrier(0);  // (left alone the compiler waits for each where it is added)
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (r + u * step < n) {
+#pragma unroll
+        for (int e = 0; e < Vec16<T>::N; ++e) acc[e] += (double)v[u].get(e);
+      }
+  }
+}
+
 // A workgroup forms the means of four neighbouring blocks of one (batch element, key head), one a wavefront: its lanes take the
-// packets of as many rows at a time as they cover. Sums are in 64 bits: those of bf16 keys are then exact.
+// packets of as many rows at a time as they cover.
 template <class T>
 __global__ __launch_bounds__(256) void block_means_kernel(const T* __restrict__ k, lc_strides ks, const int32_t* __restrict__ k_len,
                                                           double* __restrict__ means, int Tk, int Hkv, int d, int block, int nk,
@@ -140,14 +160,7 @@ __global__ __launch_bounds__(256) void block_means_kernel(const T* __restrict__ 
   double acc[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) acc[e] = 0.0;
-  if (r0 < rows) {
-    const T* const base = k + b * ks.batch + h * ks.head + pk * VEC;
-    for (int r = r0; r < n; r += rows) {
-      const Vec16<T> v = load16(base + (int64_t)(t0 + r) * ks.token);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] += (double)v.get(e);
-    }
-  }
+  if (r0 < rows) sum_rows(k + b * ks.batch + h * ks.head + pk * VEC + (int64_t)t0 * ks.token, ks.token, r0, rows, n, acc);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) part[wid][lane * VEC + e] = acc[e];
   __syncthreads();
@@ -182,9 +195,9 @@ __device__ __forceinline__ uint64_t order_of(double s) {
 
 // A workgroup of eight wavefronts selects for R neighbouring groups of one (batch element, head). Means of the groups' queries first,
 // 8 / R wavefronts a group; then the scores, a lane a block, RPT groups at a time (so that a mean that is read serves RPT scores),
-// into LDS as ordered numbers; then a wavefront a group searches the keep-th largest of them bit by bit and writes what is not
-// below it, by ascending block.
-template <class T, int R, int RPT>
+// into LDS as ordered numbers; then a wavefront a group searches the keep-th largest of them bit by bit, HELD of them a lane in
+// registers and the rest in LDS, and writes what is not below it, by ascending block.
+template <class T, int R, int RPT, int HELD>
 __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T* __restrict__ q, const double* __restrict__ means,
                                                            int32_t* __restrict__ index) {
   constexpr int VEC = Vec16<T>::N, WPR = 8 / R, RS = R / RPT;
@@ -207,14 +220,7 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
     double acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.0;
-    if (r0 < rows) {
-      const T* const base = q + b * a.qs.batch + h * a.qs.head + pk * VEC;
-      for (int r = r0 + (wid % WPR) * rows; r < n; r += rows * WPR) {
-        const Vec16<T> v = load16(base + (t0 + r) * a.qs.token);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] += (double)v.get(e);
-      }
-    }
+    if (r0 < rows) sum_rows(q + b * a.qs.batch + h * a.qs.head + pk * VEC + t0 * a.qs.token, a.qs.token, r0 + (wid % WPR) * rows, rows * WPR, n, acc);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) part[(wid * 64 + lane) * VEC + e] = acc[e];
   }
@@ -239,12 +245,23 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
 #pragma unroll
       for (int r = 0; r < RPT; ++r) s[r] = 0.0;
       if (j < live) {
-#pragma unroll 8
-        for (int c = 0; c < d; ++c) {
-          const double m = mb[(int64_t)c * nk + j];
+        auto batch = [&](int c0, auto n_c) {
+          constexpr int N = decltype(n_c)::value;
+          double m[N];
 #pragma unroll
-          for (int r = 0; r < RPT; ++r) s[r] = fma(qm[rs + r][c], m, s[r]);
-        }
+          for (int c = 0; c < N; ++c) m[c] = mb[(int64_t)(c0 + c) * nk + j];
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int c = 0; c < N; ++c)
+#pragma unroll
+            for (int r = 0; r < RPT; ++r) s[r] = fma(qm[rs + r][c0 + c], m[c], s[r]);
+        };
+        // Means under way at a time: few groups wait for them (2 x 4096 tokens: 32 at a time 11.5 us, eight 13.1), many would have
+        // 104 registers with 32 and two workgroups a compute unit in place of three (2 x 20011: 48 us, with eight 37)
+        int c0 = 0;
+        if (RPT <= 2)
+          for (; c0 + 32 <= d; c0 += 32) batch(c0, std::integral_constant<int, 32>{});
+        for (; c0 < d; c0 += 8) batch(c0, std::integral_constant<int, 8>{});
       }
       if (j < nk) {
 #pragma unroll
@@ -266,23 +283,73 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
   int written = 0;
   if ((int64_t)g * a.q_block < qlen) {
     const int chunks = (live + 63) / 64;
-    auto count = [&](uint64_t least) {  // blocks whose number is at least that
+    uint64_t held[HELD];
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[i] = i * 64 + lane < live ? kr[i * 64 + lane] : 0;
+    auto count = [&](uint64_t least) {  // blocks whose number is at least that (not 0)
       int n = 0;
-      for (int i = 0; i < chunks; ++i)
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (i < chunks) n += __popcll(__builtin_amdgcn_ballot_w64(held[i] >= least));
+      for (int i = HELD; i < chunks; ++i)
         n += __popcll(__builtin_amdgcn_ballot_w64(i * 64 + lane < live && kr[i * 64 + lane] >= least));
       return n;
     };
+    auto count_upper = [&](uint32_t least) {  // the same of the upper halves
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (i < chunks) n += __popcll(__builtin_amdgcn_ballot_w64((uint32_t)(held[i] >> 32) >= least));
+      for (int i = HELD; i < chunks; ++i)
+        n += __popcll(__builtin_amdgcn_ballot_w64(i * 64 + lane < live && (uint32_t)(kr[i * 64 + lane] >> 32) >= least));
+      return n;
+    };
+    // What is listed: numbers above `least`, and the first `ties` of those that equal it. Forced blocks and scores that are no
+    // numbers are counted at the ends; among the others the bits that all have in common need no search.
     uint64_t least = 1;
-    int ties = live;  // how many of those that equal `least` are taken
+    int ties = live;
     if (live > a.keep) {
-      least = 0;
-      for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t more = least | 1ull << bit;
-        const int n = count(more);
-        if (n >= a.keep) least = more;
-        if (n == a.keep) break;
+      const int forced = count(~0ull), real = count(2) - forced, want = a.keep - forced;
+      if (want <= 0) {
+        least = ~0ull;
+        ties = a.keep;
+      } else if (real <= want) {
+        ties = want - real;
+      } else {
+        uint64_t all = ~0ull, any = 0;
+        auto look = [&](uint64_t v) {
+          if (v > 1 && v != ~0ull) {
+            all &= v;
+            any |= v;
+          }
+        };
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+          if (i < chunks) look(held[i]);
+        for (int i = HELD; i < chunks; ++i) look(i * 64 + lane < live ? kr[i * 64 + lane] : 0);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          all &= (uint64_t)__shfl_xor((long long)all, o, 64);
+          any |= (uint64_t)__shfl_xor((long long)any, o, 64);
+        }
+        least = all;
+        ties = want;  // (all of them equal: the first ones)
+        if (all != any) {
+          int bit = 63 - __builtin_clzll(all ^ any), n = 0;
+          least = any >> bit >> 1 << bit << 1;
+          for (; bit >= 32 && n != a.keep; --bit) {  // (the upper halves nearly always tell)
+            const uint64_t more = least | 1ull << bit;
+            n = count_upper((uint32_t)(more >> 32));
+            if (n >= a.keep) least = more;
+          }
+          for (; bit >= 0 && n != a.keep; --bit) {
+            const uint64_t more = least | 1ull << bit;
+            n = count(more);
+            if (n >= a.keep) least = more;
+          }
+          ties = a.keep - count(least + 1);
+        }
       }
-      ties = a.keep - (least == ~0ull ? 0 : count(least + 1));
     }
     for (int i = 0; i < chunks; ++i) {
       const int j = i * 64 + lane;
@@ -493,20 +560,21 @@ lc_status lc_op_block_select(const lc_sparse_args* a, const void* q, const doubl
   if (blocks > (int64_t)1 << 22) return bad(LC_ERR_SHAPE, "too many groups of queries");
   const size_t sums = (size_t)8 * 64 * (a->dtype == LC_BF16 ? 8 : 4) * 8, nums = (size_t)R * k.nk * 8;
   const size_t lds = (size_t)R * 128 * 8 + (sums > nums ? sums : nums);
-#define LC_RUN(T, R_, P_)                                                                                                          \
+#define LC_RUN(T, R_, P_, N_)                                                                                                      \
   do {                                                                                                                             \
-    const hipError_t e = lds <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)block_select_kernel<T, R_, P_>,              \
+    const hipError_t e = lds <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)block_select_kernel<T, R_, P_, N_>,          \
                                                                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);    \
     if (e != hipSuccess) return (lc_status)op_fail(LC_ERR_HIP, "block_select: %s", hipGetErrorString(e));                          \
-    block_select_kernel<T, R_, P_><<<(unsigned)blocks, 512, lds, (hipStream_t)stream>>>(k, (const T*)q, means, index);             \
+    block_select_kernel<T, R_, P_, N_><<<(unsigned)blocks, 512, lds, (hipStream_t)stream>>>(k, (const T*)q, means, index);         \
   } while (0)
-#define LC_GO(R_, P_) do { if (a->dtype == LC_BF16) LC_RUN(bf16_t, R_, P_); else LC_RUN(float, R_, P_); } while (0)
-  // groups a lane scores at once: as many as leave every wavefront blocks of its own
+#define LC_GO(R_, P_, N_) do { if (a->dtype == LC_BF16) LC_RUN(bf16_t, R_, P_, N_); else LC_RUN(float, R_, P_, N_); } while (0)
+  // Groups a lane scores at once: what this is bound by is L2, which every means goes through once for them all (2 x 20011 tokens, 313
+  // blocks: 8 groups 36.5 us, 4 groups 39.3), but not so many that few wavefronts have blocks
   const int chunks = (k.nk + 63) / 64;
-  if (R == 8) { if (chunks >= 8) LC_GO(8, 8); else if (chunks >= 4) LC_GO(8, 4); else if (chunks >= 2) LC_GO(8, 2); else LC_GO(8, 1); }
-  else if (R == 4) { if (chunks >= 8) LC_GO(4, 4); else if (chunks >= 4) LC_GO(4, 2); else LC_GO(4, 1); }
-  else if (R == 2) { if (chunks >= 8) LC_GO(2, 2); else LC_GO(2, 1); }
-  else LC_GO(1, 1);
+  if (R == 8) { if (chunks >= 4) LC_GO(8, 8, 8); else if (chunks >= 2) LC_GO(8, 2, 3); else LC_GO(8, 1, 1); }
+  else if (R == 4) { if (chunks >= 8) LC_GO(4, 4, 8); else if (chunks >= 4) LC_GO(4, 2, 8); else LC_GO(4, 1, 3); }
+  else if (R == 2) { if (chunks >= 8) LC_GO(2, 2, 8); else if (chunks >= 2) LC_GO(2, 1, 8); else LC_GO(2, 1, 1); }
+  else { if (chunks >= 2) LC_GO(1, 1, 8); else LC_GO(1, 1, 1); }
 #undef LC_GO
 #undef LC_RUN
   return launched("block_select");
