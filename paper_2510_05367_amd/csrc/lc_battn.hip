@@ -22,12 +22,26 @@ namespace {
 typedef __attribute__((address_space(3))) unsigned char* lds_ptr;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
+// Division of numbers below 2^31 by one that the host knows: a multiplication (the compiler's division is some thirty
+// instructions, and a workgroup finds its place with seven of them)
+struct Div {
+  uint32_t d, m, s;
+  Div() = default;
+  explicit Div(int64_t by) : d((uint32_t)by), s(0) {
+    while (s < 31 && (1u << s) < d) ++s;
+    m = (uint32_t)((((uint64_t)1 << 32) * ((1u << s) - d)) / d + 1);
+  }
+  __device__ __forceinline__ uint32_t quot(uint32_t n) const { return (uint32_t)(((uint64_t)__umulhi(m, n) + n) >> s); }
+};
+
 struct BlockAttnArgs {
+  Div per_run, per_prob, by_splits, by_parts, by_H, by_group;  // workgroups of `unit` heads, of one; .. heads that share a key head
   lc_strides qs, ks, vs, os;
   const int32_t *index, *q_len, *k_len;
   float* part;      // several workgroups a list: [query of all][split][D] sums, then [query of all][split][2] maxima and denominators
   float scale;      // of a score, to log2 units
-  int B, Tq, Tk, H, Hkv, block, q_block, keep, nq, splits;
+  int B, Tq, Tk, H, Hkv, block, q_block, keep, nq;
+  int parts, splits; // workgroups of a group: for 128 / KS of its queries each, and for a share of its list each
   int unit;         // heads in a row that go to one XCD (0: workgroups are dealt out as they come)
 };
 
@@ -67,33 +81,35 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
   const int lq = lane & 31, hh = lane >> 5;
   // Workgroups are handed to the XCDs in turn: all that read the same keys and values (the groups of a head, and the heads that
   // share it) are put on one, whose L2 then fetches them once
-  int prob, in;
-  {
-    const int per = a.nq * a.splits, run = a.unit * per, id = blockIdx.x;
-    if (a.unit > 0) {
-      const int slot = id >> 3, u8 = slot / run, w = slot - u8 * run, p = w / per;
-      prob = ((id & 7) + 8 * u8) * a.unit + p;
-      in = w - p * per;
-    } else {
-      prob = id / per;
-      in = id - prob * per;
-    }
+  uint32_t prob, in = blockIdx.x;
+  if (a.unit > 0) {
+    const uint32_t slot = in >> 3, u8 = a.per_run.quot(slot), w = slot - u8 * a.per_run.d, p = a.per_prob.quot(w);
+    prob = ((in & 7) + 8 * u8) * a.unit + p;
+    in = w - p * a.per_prob.d;
+  } else {
+    prob = a.per_prob.quot(in);
+    in -= prob * a.per_prob.d;
   }
-  const int split = in % a.splits, g = in / a.splits, b = prob / a.H, h = prob - b * a.H, hk = h / (a.H / a.Hkv);
-  const int TK = a.k_len ? min(max(a.k_len[b], 0), a.Tk) : a.Tk;
-  const int row0 = g * a.q_block, rows = min(min(a.q_len ? max(a.q_len[b], 0) : a.Tq, a.Tq) - row0, a.q_block);
-  if (rows <= 0) return;
+  const int gp = (int)a.by_splits.quot(in), split = (int)in - gp * a.splits, g = (int)a.by_parts.quot(gp), part = gp - g * a.parts;
+  const int b = (int)a.by_H.quot(prob), h = (int)prob - b * a.H, hk = (int)a.by_group.quot(h);
   const int32_t* const list = a.index + ((int64_t)prob * a.nq + g) * a.keep;
   int ent = list[min(lane, a.keep - 1)];  // a lane holds an entry of the list, 64 at a time
+  const int row0 = g * a.q_block + part * (128 / KS);            // first query
+  const int most = min(a.Tq - row0, min(a.q_block - part * (128 / KS), 128 / KS));  // and how many there could be
 
-  // ---- queries: B operand of S^T = K Q^T; packets beyond D and rows beyond the group are zeros
+  // ---- queries: B operand of S^T = K Q^T; packets beyond D and rows beyond the group are zeros. (Rows behind q_len may hold anything: a
+  // query's column of everything below is its own, and theirs are not stored.)
   const int qi = wid / KS * 32 + lq;
   Vec16<T> qf[STEPS];
 #pragma unroll
   for (int j = 0; j < STEPS; ++j) {
     const int pk = 2 * j + hh;
-    qf[j] = qi < rows && pk < PK ? load16(q + b * a.qs.batch + (int64_t)(row0 + qi) * a.qs.token + h * a.qs.head + pk * VEC) : zero16<T>();
+    qf[j] = qi < most && pk < PK ? load16(q + b * a.qs.batch + (int64_t)(row0 + qi) * a.qs.token + h * a.qs.head + pk * VEC) : zero16<T>();
   }
+
+  const int TK = a.k_len ? min(max(a.k_len[b], 0), a.Tk) : a.Tk;
+  const int rows = a.q_len ? min(most, a.q_len[b] - row0) : most;
+  if (rows <= 0) return;
 
   // the list ends before its first entry that is no existing block or does not ascend
   int n = a.keep;
@@ -385,17 +401,32 @@ __global__ __launch_bounds__(256) void block_attn_join_kernel(BlockAttnArgs a, T
   if (pq >= n) return;
   const int dim = (int)(i - pq * per) * 4, prob = (int)(pq / a.Tq), row = (int)(pq - (int64_t)prob * a.Tq), b = prob / a.H, h = prob - b * a.H;
   if (a.q_len && row >= a.q_len[b]) return;
-  const float* const ml = a.part + n * a.splits * D + pq * a.splits * 2;
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  const f32x2* const ml = reinterpret_cast<const f32x2*>(a.part + n * a.splits * D) + pq * a.splits;
   const float* const po = a.part + pq * a.splits * D + dim;
   float top = -INFINITY, l = 0.f;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[2 * s]);
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float f = ml[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2 * s] - top);
-    l += ml[2 * s + 1] * f;
-    const f32x4 v = *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
+  constexpr int AHEAD = 4;  // splits under way at a time
+  for (int s0 = 0; s0 < a.splits; s0 += AHEAD) {
+    f32x2 w[AHEAD];
+    f32x4 v[AHEAD];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[e], f, acc[e]);
+    for (int u = 0; u < AHEAD; ++u) {
+      const int s = min(s0 + u, a.splits - 1);
+      w[u] = ml[s];
+      v[u] = *reinterpret_cast<const f32x4*>(po + (int64_t)s * D);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (s0 + u >= a.splits) break;
+      const float t = fmaxf(top, w[u][0]);
+      const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - t), g = w[u][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w[u][0] - t);
+      top = t;
+      l = l * f + w[u][1] * g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = acc[e] * f + v[u][e] * g;
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* const orow = out + b * a.os.batch + (int64_t)row * a.os.token + h * a.os.head + dim;
@@ -403,20 +434,25 @@ __global__ __launch_bounds__(256) void block_attn_join_kernel(BlockAttnArgs a, T
   for (int e = 0; e < 4; ++e) orow[e] = from_f32<T>(acc[e] * inv);
 }
 
-int tiles_shared(const lc_sparse_args* a) {  // KS
-  const int rows = a->q_block < a->Tq ? a->q_block : a->Tq;
-  return rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
-}
-// Workgroups that share a list: where there are too few groups for the chip, as many as leave each of them a few stages
-int list_splits(const lc_sparse_args* a) {
+struct AttnSplit { int ks, parts, splits; };
+// How a call is shared out. Groups of up to 32, 64, 128 queries take 4, 2, 1 wavefronts a tile. Where that leaves compute units
+// without work, bf16 groups are cut into parts of fewer tiles, whose keys more wavefronts share (16 heads of 64, 512 queries, 32 of 128
+// blocks: 17.8 us, with the lists cut instead 16.7 + 4.5 for the join; floats, whose stages are twice as long, gain nothing), and then
+// lists among several workgroups, as long as each of them keeps two stages (16 heads, one query, 32 blocks: 7.0 us with two, 8.8 with
+// four, 17 uncut; 4 heads of floats, 300 queries, 20 blocks: 12.6, 16.6 and 53).
+AttnSplit attn_split(const lc_sparse_args* a) {
   const int64_t groups = (int64_t)a->B * a->heads * lc_sparse_groups(a);
-  const int64_t cpb = a->block / 64, most = ((int64_t)a->Tk + 63) / 64;
-  const int64_t chunks = a->keep * cpb < most ? a->keep * cpb : most;
-  const int64_t stages = tiles_shared(a) == 4 ? (chunks + 1) / 2 : chunks;
-  if (groups >= 256) return 1;
-  const int64_t want = (512 + groups - 1) / groups, room = stages / 4;
-  const int64_t s = want < room ? want : room;
-  return s < 1 ? 1 : (int)s;
+  const int rows = a->q_block < a->Tq ? a->q_block : a->Tq;
+  AttnSplit r;
+  r.ks = rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+  if (a->dtype == LC_BF16)
+    while (r.ks < 4 && groups * ((rows * r.ks + 127) / 128) < 512) r.ks *= 2;
+  r.parts = (rows * r.ks + 127) / 128;
+  const int64_t wgs = groups * r.parts, cpb = a->block / 64, most = ((int64_t)a->Tk + 63) / 64;
+  const int64_t chunks = a->keep * cpb < most ? a->keep * cpb : most, stages = r.ks == 4 ? (chunks + 1) / 2 : chunks;
+  const int64_t want = wgs < 256 ? (512 + wgs - 1) / wgs : 1, room = stages / 2, s = want < room ? want : room;
+  r.splits = s < 1 ? 1 : (int)s;
+  return r;
 }
 
 int check_attention(const lc_sparse_args* a) {
@@ -446,7 +482,7 @@ template <class T, int D, int KS> hipError_t run_block_attn(hipStream_t s, const
       done.fetch_or(bit);
     }
   }
-  const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nq * a.splits);
+  const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.nq * a.parts * a.splits);
   block_attn_kernel<T, D, KS><<<grid, 256, lds, s>>>(a, (const T*)q, (const T*)k, (const T*)v, (T*)out);
   return hipGetLastError();
 }
@@ -477,7 +513,7 @@ extern "C" {
 
 size_t lc_block_attention_workspace(const lc_sparse_args* a) {
   if (check_attention(a) != LC_OK) return 0;
-  const int s = list_splits(a);
+  const int s = attn_split(a).splits;
   return s == 1 ? 0 : (size_t)a->B * a->heads * a->Tq * s * (a->head_dim + 2) * 4;
 }
 
@@ -501,12 +537,16 @@ lc_status lc_op_block_attention(const lc_sparse_args* a, const void* q, const vo
   k_.part = (float*)workspace;
   k_.scale = a->q_prescaled ? 1.f : attn_q_scale(a->head_dim);
   k_.B = a->B; k_.Tq = a->Tq; k_.Tk = a->Tk; k_.H = a->heads; k_.Hkv = a->kv_heads; k_.block = a->block; k_.q_block = a->q_block;
-  k_.keep = a->keep; k_.nq = lc_sparse_groups(a); k_.splits = list_splits(a);
+  k_.keep = a->keep; k_.nq = lc_sparse_groups(a);
+  const AttnSplit sp = attn_split(a);
+  k_.splits = sp.splits; k_.parts = sp.parts;
   const int64_t kvs = (int64_t)a->B * a->kv_heads;
   k_.unit = kvs % 8 == 0 ? a->heads / a->kv_heads : kvs * (a->heads / a->kv_heads) % 8 == 0 ? 1 : 0;
-  const int ks = tiles_shared(a);
-  hipError_t e = a->dtype == LC_BF16 ? block_attn_dispatch<bf16_t>((hipStream_t)stream, k_, a->head_dim, ks, q, k, v, out)
-                                     : block_attn_dispatch<float>((hipStream_t)stream, k_, a->head_dim, ks, q, k, v, out);
+  const int64_t per = (int64_t)k_.nq * k_.parts * k_.splits;
+  k_.per_prob = Div(per); k_.per_run = Div(per * (k_.unit > 0 ? k_.unit : 1));
+  k_.by_splits = Div(k_.splits); k_.by_parts = Div(k_.parts); k_.by_H = Div(k_.H); k_.by_group = Div(k_.H / k_.Hkv);
+  hipError_t e = a->dtype == LC_BF16 ? block_attn_dispatch<bf16_t>((hipStream_t)stream, k_, a->head_dim, sp.ks, q, k, v, out)
+                                     : block_attn_dispatch<float>((hipStream_t)stream, k_, a->head_dim, sp.ks, q, k, v, out);
   if (e == hipSuccess && k_.splits > 1) {
     const int64_t n = (int64_t)a->B * a->heads * a->Tq * (a->head_dim / 4);
     const unsigned blocks = (unsigned)((n + 255) / 256);
