@@ -584,7 +584,7 @@ lc_status lc_op_rope(const lc_rope_table* table /* [host] */, const lc_rope_args
  * the group's queries and of the block's keys; a list holds the `keep` blocks of the highest scores. Query head h reads key
  * head h / (heads / kv_heads).
  * Requirements (else LC_ERR_SHAPE): sizes > 0; heads a multiple of kv_heads; head_dim in {8, 16, 32, 40, 64, 128}; block a
- * multiple of 64; 1 <= q_block <= 128; keep <= 65536; at most 8192 blocks; strides and pointers of q, k, v and out such that every
+ * multiple of 64, at most 2^20; 1 <= q_block <= 128; keep <= 65536; Tk <= 2^30; at most 8192 blocks; strides and pointers of q, k, v and out such that every
  * head's row is 16-byte aligned; 64 token strides of k and v within 2^30 bytes. */
 typedef struct lc_sparse_args {
   int32_t B, Tq, Tk, heads, kv_heads, head_dim, dtype;
@@ -627,7 +627,7 @@ typedef enum { LC_ENTRY_PLAIN = -1, LC_ENTRY_INT8 = 0, LC_ENTRY_FP8 = 1, LC_ENTR
 typedef struct lc_entry_args {
   int32_t format;          /* lc_entry_format, not LC_ENTRY_PLAIN */
   int32_t cols;
-  int64_t rows;
+  int64_t rows;            /* in all less than 2^34 values, counting whole groups */
   int32_t x_dtype, y_dtype; /* lc_dtype of x; of base and y */
   int64_t x_ld, y_ld;      /* elements from one row to the next: of x; of base and y */
 } lc_entry_args;

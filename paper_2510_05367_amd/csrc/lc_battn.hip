@@ -16,6 +16,7 @@ namespace lc {
 
 int check_sparse_args(const lc_sparse_args* a);  // lc_tokens.hip
 int check_sparse_rows(const char* name, const void* p, const lc_strides& s, int dt);
+bool strides_apart(const lc_strides& s, int B, int T, int heads);
 
 namespace {
 
@@ -458,10 +459,10 @@ AttnSplit attn_split(const lc_sparse_args* a) {
 int check_attention(const lc_sparse_args* a) {
   int s = check_sparse_args(a);
   if (s != LC_OK) return s;
-  if (a->Tk > 1 << 30 || a->block > 1 << 20) return op_fail(LC_ERR_SHAPE, "Tk must be at most 2^30 and block at most 2^20");
   const int64_t es = (int64_t)dtype_size(a->dtype), most = ((int64_t)1 << 30) / 64 / es;
   if (a->k.token > most || a->v.token > most || a->k.token < 0 || a->v.token < 0) return op_fail(LC_ERR_SHAPE, "64 token strides of k and v must be within 2^30 bytes");
   if (a->Tk > 1 && (a->k.token < a->head_dim || a->v.token < a->head_dim)) return op_fail(LC_ERR_SHAPE, "the rows of k and of v must not overlap");
+  if (!strides_apart(a->out, a->B, a->Tq, a->heads)) return op_fail(LC_ERR_SHAPE, "the rows of out must not overlap");
   const int64_t groups = (int64_t)a->B * a->heads * lc_sparse_groups(a);
   if (groups > (int64_t)1 << 23) return op_fail(LC_ERR_SHAPE, "too many groups of queries");
   return LC_OK;

@@ -116,12 +116,12 @@ template <int F> __device__ __forceinline__ uint32_t get_codes(const unsigned ch
 template <int F, class X, class Y, bool WHOLE>
 __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_ld, unsigned char* __restrict__ codes,
                                                          unsigned char* __restrict__ scales, const Y* base, Y* y, int64_t y_ld,
-                                                         int64_t packets, uint32_t ppr, int cols) {
+                                                         uint32_t packets, uint32_t ppr, int cols) {
   typedef Code<F> C;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   const bool live = i < packets;  // (the eight threads of a group are all alive or all not)
   const int64_t row = live ? i / ppr : 0;
-  const int c0 = (int)(live ? i - row * ppr : 0) * 4;
+  const int c0 = live ? (int)(i % ppr) * 4 : 0;
   const int left = live ? cols - c0 : 0;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (left > 0) load4<X, WHOLE>(x + row * x_ld + c0, left, v);
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_l
   for (int e = 0; e < 4; ++e) u[e] = number ? v[e] * down : 0.f;
   const uint32_t w = C::pack4(u);
   if (!live) return;
-  put_codes<F>(codes + i * (C::kBits / 2), w);
+  put_codes<F>(codes + (int64_t)i * (C::kBits / 2), w);
   if ((threadIdx.x & 7) == 0) scales[i >> 3] = (unsigned char)byte;
   if (y != nullptr && left > 0) {
     const float up = scale_up(byte);
@@ -154,16 +154,16 @@ __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_l
 
 template <int F, class Y, bool WHOLE>
 __global__ __launch_bounds__(256) void entry_unpack_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
-                                                           const Y* base, Y* y, int64_t y_ld, int64_t packets, uint32_t ppr, int cols) {
+                                                           const Y* base, Y* y, int64_t y_ld, uint32_t packets, uint32_t ppr, int cols) {
   typedef Code<F> C;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   if (i >= packets) return;
   const int64_t row = i / ppr;
-  const int c0 = (int)(i - row * ppr) * 4, left = cols - c0;
+  const int c0 = (int)(i % ppr) * 4, left = cols - c0;
   if (left <= 0) return;
   float u[4], b[4] = {0.f, 0.f, 0.f, 0.f};
   if (base != nullptr) load4<Y, WHOLE>(base + row * y_ld + c0, left, b);
-  C::unpack4(get_codes<F>(codes + i * (C::kBits / 2)), u);
+  C::unpack4(get_codes<F>(codes + (int64_t)i * (C::kBits / 2)), u);
   const float up = scale_up(scales[i >> 3]);
 #pragma unroll
   for (int e = 0; e < 4; ++e) b[e] += u[e] * up;
@@ -175,7 +175,7 @@ struct EntryShape { int64_t groups, packets, code_bytes, total; };
 bool entry_shape(const lc_entry_args* a, EntryShape* s) {
   if (!a || a->format < LC_ENTRY_INT8 || a->format > LC_ENTRY_FP4 || a->rows <= 0 || a->cols <= 0) return false;
   const int64_t groups = ((int64_t)a->cols + kGroup - 1) / kGroup;
-  if (a->rows > ((int64_t)1 << 38) / groups) return false;  // (offsets stay far from the end of 64 bits)
+  if (a->rows > (((int64_t)1 << 29) - 64) / groups) return false;  // (packets of four values are counted, and launched, in 32 bits)
   s->groups = groups;
   s->packets = a->rows * groups * (kGroup / 4);
   s->code_bytes = a->rows * groups * (a->format == LC_ENTRY_FP4 ? kGroup / 2 : kGroup);
@@ -193,7 +193,7 @@ lc_status bad(int status, const char* what) { return (lc_status)op_fail(status, 
 lc_status check_entry(const lc_entry_args* a, const void* entry, EntryShape* s) {
   if (!a) return bad(LC_ERR_ARG, "args is NULL");
   if (a->format < LC_ENTRY_INT8 || a->format > LC_ENTRY_FP4) return bad(LC_ERR_ARG, "format must be one of LC_ENTRY_INT8, LC_ENTRY_FP8, LC_ENTRY_FP4");
-  if (!entry_shape(a, s)) return bad(LC_ERR_SHAPE, "rows and cols must be positive, and of at most 2^43 values");
+  if (!entry_shape(a, s)) return bad(LC_ERR_SHAPE, "rows and cols must be positive, and of less than 2^34 values in all");
   if (!entry) return bad(LC_ERR_ARG, "entry is NULL");
   if ((uintptr_t)entry % 16) return bad(LC_ERR_ARG, "entry must be 16-byte aligned");
   return LC_OK;
@@ -230,7 +230,7 @@ lc_status lc_op_entry_pack(const lc_entry_args* a, const void* x, void* entry, c
   const unsigned blocks = (unsigned)((s.packets + 255) / 256);
 #define LC_GO(F, X, Y, W)                                                                                                            \
   entry_pack_kernel<F, X, Y, W><<<blocks, 256, 0, (hipStream_t)stream>>>((const X*)x, a->x_ld, codes, codes + s.code_bytes, (const Y*)base, \
-                                                                         (Y*)y, a->y_ld, s.packets, (uint32_t)(s.groups * (kGroup / 4)), a->cols)
+                                                                         (Y*)y, a->y_ld, (uint32_t)s.packets, (uint32_t)(s.groups * (kGroup / 4)), a->cols)
 #define LC_W(F, X, Y) do { if (whole) LC_GO(F, X, Y, true); else LC_GO(F, X, Y, false); } while (0)
 #define LC_T(F)                                                                                   \
   do {                                                                                            \
@@ -260,7 +260,7 @@ lc_status lc_op_entry_unpack(const lc_entry_args* a, const void* entry, const vo
   const unsigned char* const codes = (const unsigned char*)entry;
   const unsigned blocks = (unsigned)((s.packets + 255) / 256);
 #define LC_GO(F, Y, W)                                                                                                                   \
-  entry_unpack_kernel<F, Y, W><<<blocks, 256, 0, (hipStream_t)stream>>>(codes, codes + s.code_bytes, (const Y*)base, (Y*)y, a->y_ld, s.packets, \
+  entry_unpack_kernel<F, Y, W><<<blocks, 256, 0, (hipStream_t)stream>>>(codes, codes + s.code_bytes, (const Y*)base, (Y*)y, a->y_ld, (uint32_t)s.packets, \
                                                                         (uint32_t)(s.groups * (kGroup / 4)), a->cols)
 #define LC_W(F, Y) do { if (whole) LC_GO(F, Y, true); else LC_GO(F, Y, false); } while (0)
 #define LC_T(F) do { if (a->y_dtype == LC_F32) LC_W(F, float); else LC_W(F, bf16_t); } while (0)

@@ -380,9 +380,14 @@ int check_sparse_args(const lc_sparse_args* a) {
   if (a->block <= 0 || a->block % 64) return bad(LC_ERR_SHAPE, "block must be a positive multiple of 64");
   if (a->q_block < 1 || a->q_block > 128) return bad(LC_ERR_SHAPE, "q_block must be in [1, 128]");
   if (a->keep < 1 || a->keep > 65536) return bad(LC_ERR_SHAPE, "keep must be in [1, 65536]");
+  if (a->Tk > 1 << 30 || a->block > 1 << 20) return bad(LC_ERR_SHAPE, "Tk must be at most 2^30 and block at most 2^20");
   if (((int64_t)a->Tk + a->block - 1) / a->block > 8192) return bad(LC_ERR_SHAPE, "more than 8192 key blocks: use larger ones");
-  if ((int64_t)a->B * a->heads * a->Tq > (int64_t)1 << 40) return bad(LC_ERR_SHAPE, "too many queries");
+  if ((int64_t)a->B * a->heads > 1 << 24) return bad(LC_ERR_SHAPE, "at most 2^24 heads of all batch elements");
   return LC_OK;
+}
+// an output: no axis of stride zero
+bool strides_apart(const lc_strides& s, int B, int T, int heads) {
+  return (B == 1 || s.batch != 0) && (T == 1 || s.token != 0) && (heads == 1 || s.head != 0);
 }
 // one strided input or output whose rows are moved in 16-byte packets
 int check_sparse_rows(const char* name, const void* p, const lc_strides& s, int dt) {
@@ -447,6 +452,7 @@ lc_status lc_op_rope(const lc_rope_table* t, const lc_rope_args* a, const void* 
   if (a->B <= 0 || a->T <= 0 || a->heads <= 0) return bad(LC_ERR_SHAPE, "all sizes must be positive");
   if (a->inverse != 0 && a->inverse != 1) return bad(LC_ERR_ARG, "inverse must be 0 or 1");
   if (a->heads > 1 << 20 || a->T > 1 << 27) return bad(LC_ERR_SHAPE, "at most 2^20 heads and 2^27 tokens");
+  if (!strides_apart(a->y, a->B, a->T, a->heads)) return bad(LC_ERR_SHAPE, "the rows of y must not overlap");
   RopeArgs k;
   k.xs = a->x; k.ys = a->y;
   k.T = a->T; k.H = a->heads; k.axes = t->axes; k.pairs = t->rot_dim / 2; k.rot = t->rot_dim;

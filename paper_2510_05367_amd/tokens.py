@@ -43,13 +43,13 @@ def _launch(device, call, *args):
             call(*args, torch._C._cuda_getCurrentRawStream(i))
 
 
-def _on(device, **tensors):
+def _on(device, *tensors):
     """The tensors that are given are on that GPU."""
     if device.type != "cuda":
         raise ValueError("tensors must be on a GPU (there is no CPU fallback)")
-    for name, t in tensors.items():
+    for t in tensors:
         if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+            raise ValueError(f"tensors on {device} and on {t.device}")
 
 
 def _strides(name, shape, stride):
@@ -116,13 +116,13 @@ def rope(x, table: lcb.lc_rope_table, pos=None, grid: Optional[Sequence[int]] = 
         B, T = x.shape[:2]
         if grid is not None or any(starts):
             raise ValueError("pos holds the positions: no grid and no start beside it")
-        if n == 1 and pos.shape[-1:] != (1,) or pos.dim() == 1:
+        if n == 1 and tuple(pos.shape) in ((T,), (B, T)) and tuple(pos.shape) != (T, 1):
             pos = pos.unsqueeze(-1)
         if pos.dtype != torch.int32 or not pos.is_contiguous() or tuple(pos.shape) not in ((T, n), (B, T, n)):
             raise ValueError(f"pos must be contiguous int32 of shape {(T, n)} or {(B, T, n)}")
         pos_batch = T * n if pos.dim() == 3 else 0
     a = _rope_args(x.shape, x.stride(), out.stride(), x.dtype, n, None if grid is None else tuple(grid), starts, bool(inverse), pos_batch)
-    _on(x.device, out=out, pos=pos)
+    _on(x.device, out, pos)
     if x.numel() == 0:
         return out
     _launch(x.device, lcb.lc_op_rope, table, a, x.data_ptr(), _ptr(pos), out.data_ptr())
@@ -148,7 +148,7 @@ def block_means(k, block: int = 64, k_len=None, first: int = 0, count: Optional[
     count = nk - first if count is None else count
     if out is None and (first, count) != (0, nk):
         raise ValueError("some blocks of a tensor: give the tensor")
-    _on(k.device, k_len=k_len, out=out)
+    _on(k.device, k_len, out)
     out = _out(out, (B, Hkv, d, nk), torch.float64, k.device)
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
@@ -173,7 +173,7 @@ def block_select(q, means, Tk: int, keep: int, block: int = 64, q_block: int = 1
     B = q.shape[0]
     if means.dtype != torch.float64 or not means.is_contiguous():
         raise ValueError("means must be what block_means made")
-    _on(q.device, means=means, q_len=q_len, k_len=k_len, out=out)
+    _on(q.device, means, q_len, k_len, out)
     out = _out(out, shape, torch.int32, q.device)
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
@@ -198,7 +198,7 @@ def _select_args(shape, stride, dtype, m_shape, Tk, keep, block, q_block, sink, 
 def block_attention(q, k, v, index, block: int = 64, q_block: int = 128, q_len=None, k_len=None, q_prescaled: bool = False, out=None):
     """Attention of q [B, Tq, heads, head_dim] over the keys and values [B, Tk, kv_heads, head_dim] of the blocks that ``index`` (int32
     [B, heads, groups, keep], of :func:`block_select` or of the caller's own) lists for each group of q_block queries."""
-    _on(q.device, k=k, v=v, index=index, q_len=q_len, k_len=k_len, out=out)
+    _on(q.device, k, v, index, q_len, k_len, out)
     out = _out(out, q.shape, q.dtype, q.device)
     a, groups, need = _attention_args(q.shape, q.stride(), q.dtype, k.shape, k.stride(), v.shape, v.stride(), out.stride(), index.shape,
                                       block, q_block, bool(q_prescaled))
@@ -235,7 +235,7 @@ def entry_pack(x, fmt: str, base=None, out=None, entry=None):
     """Writes x [rows, cols] into an entry (uint8; ``entry``, or a new one, which is returned). With ``out`` [rows, cols] also
     out = base + what the entry stands for (base None: zeros), in the same pass."""
     a, need = _entry_args(fmt, x.shape, x.stride(), x.dtype, *_rest(base, out))
-    _on(x.device, base=base, out=out, entry=entry)
+    _on(x.device, base, out, entry)
     entry = _out(entry, (need,), torch.uint8, x.device, "entry")
     if not entry.is_contiguous():
         raise ValueError("entry must be contiguous")
@@ -245,7 +245,7 @@ def entry_pack(x, fmt: str, base=None, out=None, entry=None):
 
 def entry_unpack(entry, rows: int, cols: int, fmt: str, base=None, out=None, dtype=torch.float32):
     """out [rows, cols] = base + the values of an entry (base None: zeros)."""
-    _on(entry.device, base=base, out=out)
+    _on(entry.device, base, out)
     if out is None:
         out = torch.empty(rows, cols, dtype=dtype if base is None else base.dtype, device=entry.device)
     a, need = _entry_args(fmt, (rows, cols), None, None, *_rest(base, out))

@@ -75,6 +75,8 @@ def test_rope_pointers_tables_and_grids():
     refused(1, "lc_rope_make", lambda: lcb.lc_op_rope(lcb.lc_rope_table(), rope_args(), P, None, 2 * P, None))
     refused(2, "same strides", lambda: lcb.lc_op_rope(t, rope_args(y=lcb.lc_strides(512, 64, 256)), P, None, P, None))
     refused(2, "grid", lambda: lcb.lc_op_rope(tokens.make_rope(64, axes=(32, 32)), rope_args(), P, None, 2 * P, None))
+    for y in (lcb.lc_strides(0, 128, 64), lcb.lc_strides(512, 0, 64), lcb.lc_strides(512, 128, 0)):
+        refused(2, "overlap", lambda: lcb.lc_op_rope(t, rope_args(B=2, y=y), P, None, 2 * P, None))
     t.axis_dim[0] = 32
     refused(1, "lc_rope_make", lambda: lcb.lc_op_rope(t, rope_args(), P, None, 2 * P, None))
 
@@ -90,7 +92,8 @@ def sparse_args(**kw):
 BAD_SPARSE = [(dict(B=0), 2, "positive"), (dict(Tq=0), 2, "positive"), (dict(Tk=0), 2, "positive"), (dict(heads=3), 2, "multiple of kv_heads"),
               (dict(kv_heads=0), 2, "positive"), (dict(head_dim=24), 2, "head_dim"), (dict(dtype=7), 1, "dtype"), (dict(block=0), 2, "block"),
               (dict(block=96), 2, "block"), (dict(block=-64), 2, "block"), (dict(q_block=0), 2, "q_block"), (dict(q_block=129), 2, "q_block"),
-              (dict(keep=0), 2, "keep"), (dict(keep=65537), 2, "keep"), (dict(Tk=64 * 8192 + 1), 2, "8192")]
+              (dict(keep=0), 2, "keep"), (dict(keep=65537), 2, "keep"), (dict(Tk=64 * 8192 + 1), 2, "8192"),
+              (dict(Tk=(1 << 30) + 1), 2, "2^30"), (dict(block=1 << 21), 2, "2^20"), (dict(B=(1 << 31) - 1, heads=(1 << 31) - 1, kv_heads=1), 2, "2^24")]
 means_call = lambda a: lcb.lc_op_block_means(a, P, None, P, 0, 1, None)  # noqa: E731
 select_call = lambda a: lcb.lc_op_block_select(a, P, P, None, None, P, None)  # noqa: E731
 attend_call = lambda a: lcb.lc_op_block_attention(a, P, P, P, P, None, None, P, P, 1 << 40, None)  # noqa: E731
@@ -128,6 +131,7 @@ def test_sparse_pointers_ranges_and_workspaces():
     refused(2, "overlap", lambda: attend_call(sparse_args(k=lcb.lc_strides(1000 * 128, 56, 64))))
     refused(2, "2^30", lambda: attend_call(sparse_args(v=lcb.lc_strides(0, 1 << 24, 64))))
     refused(2, "2^30", lambda: attend_call(sparse_args(k=lcb.lc_strides(0, -128, 64))))
+    refused(2, "overlap", lambda: attend_call(sparse_args(out=lcb.lc_strides(0, 128, 64))))
     few = sparse_args(Tq=1, keep=16)
     need = lcb.lc_block_attention_workspace(few)
     assert need > 0 and need % (2 * 2 * 1 * 66 * 4) == 0
@@ -150,7 +154,7 @@ def test_entries():
     for call in (pack, unpack):
         for f in (-1, 3):
             refused(1, "format", lambda: call(entry_args(format=f)))
-        for kw in (dict(rows=0), dict(cols=0), dict(rows=-1), dict(rows=1 << 40)):
+        for kw in (dict(rows=0), dict(cols=0), dict(rows=-1), dict(rows=1 << 40), dict(rows=(1 << 27) - 15)):
             refused(2, "rows and cols", lambda: call(entry_args(**kw)))
         refused(1, "entry is NULL", lambda: call(entry_args(), e=None))
         refused(1, "16-byte", lambda: call(entry_args(), e=P + 8))
