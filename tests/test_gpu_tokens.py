@@ -311,6 +311,9 @@ def test_attention_far_scores(dtype, Tq, q_block, spread):
     index = random_lists(rng, 1, 2, 1, 32, 32)
     ref, weight, dot = tko.block_attention(f64(q), f64(k), f64(v), index, 64, q_block)
     close(tokens.block_attention(q, k, v, ints(index.tolist()), q_block=q_block), ref, attention_bound(q, ref, weight, dot, 2048))
+    pre = (q.float() * (math.log2(math.e) / math.sqrt(32))).to(dtype)
+    ref, weight, dot = tko.block_attention(f64(pre), f64(k), f64(v), index, 64, q_block, scale=math.log(2.0))
+    close(tokens.block_attention(pre, k, v, ints(index.tolist()), q_block=q_block, q_prescaled=True), ref, attention_bound(q, ref, weight, dot, 2048))
 
 
 def test_offsets_beyond_32_bits():

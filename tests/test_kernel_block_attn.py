@@ -20,7 +20,7 @@ def attention(meta):
 
 def test_registers(asm):
     kernels = attention(asm[0])
-    assert len(kernels) == 36  # two types, six head sizes, three ways to share a tile
+    assert len(kernels) == 36 + 15  # two types, six head sizes, three ways to share a tile; prescaled queries of five sizes
     for name, (vg, scratch) in kernels.items():
         d = int(re.search(r"Li(\d+)ELi", name).group(1))
         assert scratch == 0 and vg <= (128 if d <= 64 and "DF16b" in name else 256), (name, vg, scratch)
