@@ -150,10 +150,8 @@ __global__ __launch_bounds__(256) void block_means_kernel(const T* __restrict__ 
   __shared__ double part[4][64 * VEC];
   __shared__ double mean[128][4];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  int64_t id = blockIdx.x;
-  const int q4 = (int)(id % quads);
-  id /= quads;
-  const int h = (int)(id % Hkv), b = (int)(id / Hkv);
+  // (heads first: what neighbouring workgroups read at a time are neighbouring pieces of the same rows)
+  const int h = (int)(blockIdx.x % Hkv), bq = (int)(blockIdx.x / Hkv), q4 = bq % quads, b = bq / quads;
   const int j = first + q4 * 4 + wid, len = k_len ? min(max(k_len[b], 0), Tk) : Tk;
   const int t0 = j * block, n = j < last ? min(max(len - t0, 0), block) : 0;
   const int PK = d / VEC, rows = 64 / PK, r0 = lane / PK, pk = lane - r0 * PK;
@@ -206,10 +204,8 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
   uint64_t* const keys = reinterpret_cast<uint64_t*>(smem + R * 128 * 8);   // [R][nk]; before that the sums of eight wavefronts
   double* const part = reinterpret_cast<double*>(keys);
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int64_t id = blockIdx.x;
-  const int g0 = (int)(id % a.slices) * R;
-  id /= a.slices;
-  const int h = (int)(id % a.H), b = (int)(id / a.H);
+  // (heads first: as above, and where they are a multiple of eight all groups of a head find its means in one XCD's L2)
+  const int h = (int)(blockIdx.x % a.H), bs = (int)(blockIdx.x / a.H), g0 = bs % a.slices * R, b = bs / a.slices;
   const int klen = a.k_len ? min(max(a.k_len[b], 0), a.Tk) : a.Tk, qlen = a.q_len ? min(max(a.q_len[b], 0), a.Tq) : a.Tq;
   const int d = a.d, nk = a.nk, live = (klen + a.block - 1) / a.block;
 
