@@ -609,7 +609,7 @@ lc_status lc_op_block_select(const lc_sparse_args* args, const void* q, const do
                              int32_t* index, void* stream);
 /* out[b][i][h] = softmax(q_i K^T / sqrt(head_dim)) V over the existing keys of the blocks in index[b][h][i / q_block]; zeros where
  * there are none. A list ends at its first entry that is not a block with an existing key or not greater than the entry
- * before it, so that lists of any origin are safe and no key counts twice. workspace [device, 16-byte aligned], of
+ * before it, so that lists of any origin are safe and no key counts twice. out must not overlap the inputs. workspace [device, 16-byte aligned], of
  * lc_block_attention_workspace(args) bytes (0: may be NULL): what several workgroups that share a list hand to each other; calls in
  * flight at once need one each. */
 size_t lc_block_attention_workspace(const lc_sparse_args* args); /* host only; 0 also if args are refused */

@@ -170,17 +170,17 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
     return key0;
   };
   // The requests are written out, so that the compiler does not take the transposing reads below to depend on all of them and
-  // waits for none: barrier_keep says when a stage is there. (No register is loaded, and what the descriptor is made of was written by scalar
-  // instructions; the first wait states are for those that were not.)
+  // waits for none: barrier_keep says when a stage is there. (No register is loaded. The wait states in front are what a load needs behind
+  // vector instructions that wrote its scalar operands.)
   auto issue = [&](int st, int key0) {
 #ifdef __HIP_DEVICE_COMPILE__
     const int keys = min(64, TK - key0);
     const uint64_t base = (uint64_t)(src + key0 * ld);
     typedef __attribute__((ext_vector_type(4))) int i32x4;
-    const i32x4 r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xffffu)),
+    i32x4 r = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xffffu)),
                      __builtin_amdgcn_readfirstlane(keys > 0 ? (int)(((keys - 1) * ld + D) * (int)sizeof(T)) : 0), 0x00020000};  // (raw 32-bit data)
-    const uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)(smem + (st % NB) * S::STAGE + lds_at));
-    asm volatile("s_nop 4" ::: "memory");
+    uint32_t dst = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)(smem + (st % NB) * S::STAGE + lds_at));
+    asm volatile("s_nop 4" : "+s"(r), "+s"(dst)::"memory");
 #pragma unroll
     for (int i = 0; i < LPW; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst + i * 1024), "v"(off[i]), "s"(r) : "memory");

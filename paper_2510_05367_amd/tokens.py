@@ -207,7 +207,7 @@ def block_attention(q, k, v, index, block: int = 64, q_block: int = 128, q_len=N
         raise ValueError("k and v must be of q's type")
     if index.dtype != torch.int32 or not index.is_contiguous() or index.shape[:3] != (B, H, groups):
         raise ValueError(f"index must be contiguous int32 of shape {(B, H, groups)} x keep")
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None  # (its own: captured calls share none)
     _launch(q.device, lcb.lc_op_block_attention, a, q.data_ptr(), k.data_ptr(), v.data_ptr(), index.data_ptr(), _lens("q_len", q_len, B),
             _lens("k_len", k_len, B), out.data_ptr(), _ptr(ws), need)
     return out

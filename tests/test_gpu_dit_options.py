@@ -61,6 +61,33 @@ def make(cfg, entry=None, sparse=None, axes=None, grid=None, **kw):
     return dit, w
 
 
+@pytest.mark.parametrize("B,T,D,heads,opt", [(2, 1, 256, 4, dict(sparse=dict(keep=2, sink=1), axes=(64,))), (1, 33, 320, 8, dict(sparse=dict(keep=1, q_block=1))),
+                                             (2, 65, 256, 4, dict(sparse=dict(keep=5, q_block=20), axes=(16, 24, 24), grid=(1, 7, 10)))])
+def test_few_tokens_in_a_workspace_of_nan(B, T, D, heads, opt):
+    """Every block is listed; what lies behind the tokens in the workspace is whatever was there."""
+    cfg = BF16_W.with_(B=B, T=T, D=D, heads=heads, head_dim=D // heads, L=2, cache_a=1, cache_b=2)
+    dit, w = make(cfg, entry="mxint8", **opt)
+    try:
+        x, mod = synth.make_dit_hidden(cfg, 1), synth.make_dit_modulation(cfg, 2)
+        out, again = dit.empty(*x.shape), dit.empty(*x.shape)
+        xd, md = dit.to_device(x), dit.to_device(mod)
+        dit.arena.fill_(255)
+        torch.cuda.synchronize()
+        dit.full_step(xd, md, out, 0)
+        dit.cached_step(xd, md, again, 0)
+        dit.sync()
+        assert torch.equal(out, again)
+        orc = Oracle(cfg, {k: v.astype(np.float64) for k, v in w.items()}, **opt)
+        want = orc.full_step(x, mod, 0)
+        delta = orc.dev[0].reshape(-1, D)
+        # the entry's rounding beside the step's own: half a step of 2^e, max|x| > 63.5 * 2^e
+        step = np.abs(delta).reshape(-1, D // 32, 32).max(axis=2).max() / 63.5
+        g = host(out)
+        assert np.max(np.abs(g - want)) <= 2e-2 * max(1.0, np.abs(want).max() / 4) + step / 2 + 1e-2 * np.abs(delta).max()
+    finally:
+        dit.close()
+
+
 @pytest.mark.parametrize("cfg,opt", OPTIONS)
 def test_steps_match_oracle(cfg, opt):
     dit, w = make(cfg, **opt, token_chunk=100)
