@@ -282,20 +282,20 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
     uint64_t held[HELD];
 #pragma unroll
     for (int i = 0; i < HELD; ++i) held[i] = i * 64 + lane < live ? kr[i * 64 + lane] : 0;
-    auto count = [&](uint64_t least) {  // blocks whose number is at least that (not 0)
+    auto count = [&](uint64_t least) {  // blocks whose number is at least that (not 0: lanes without a block hold it)
       int n = 0;
 #pragma unroll
       for (int i = 0; i < HELD; ++i)
-        if (i < chunks) n += __popcll(__builtin_amdgcn_ballot_w64(held[i] >= least));
+        n += __popcll(__builtin_amdgcn_ballot_w64(held[i] >= least));
       for (int i = HELD; i < chunks; ++i)
         n += __popcll(__builtin_amdgcn_ballot_w64(i * 64 + lane < live && kr[i * 64 + lane] >= least));
       return n;
     };
-    auto count_upper = [&](uint32_t least) {  // the same of the upper halves
+    auto count_upper = [&](uint32_t least) {  // the same of the upper halves (not 0)
       int n = 0;
 #pragma unroll
       for (int i = 0; i < HELD; ++i)
-        if (i < chunks) n += __popcll(__builtin_amdgcn_ballot_w64((uint32_t)(held[i] >> 32) >= least));
+        n += __popcll(__builtin_amdgcn_ballot_w64((uint32_t)(held[i] >> 32) >= least));
       for (int i = HELD; i < chunks; ++i)
         n += __popcll(__builtin_amdgcn_ballot_w64(i * 64 + lane < live && (uint32_t)(kr[i * 64 + lane] >> 32) >= least));
       return n;
@@ -320,8 +320,7 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
           }
         };
 #pragma unroll
-        for (int i = 0; i < HELD; ++i)
-          if (i < chunks) look(held[i]);
+        for (int i = 0; i < HELD; ++i) look(held[i]);
         for (int i = HELD; i < chunks; ++i) look(i * 64 + lane < live ? kr[i * 64 + lane] : 0);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
