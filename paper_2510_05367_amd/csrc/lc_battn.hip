@@ -9,8 +9,8 @@
 // transposing LDS read (bf16), so no transposed copy of V exists anywhere.
 //
 // What bounds it in large calls is the vector unit (active 67 % of the cycles) beside the matrix pipe (47 %), and a clock that falls to 1.83 GHz: 33001
-// tokens, 16 heads of 64, 64 of 516 blocks 598 us = 925 TFLOP/s (a large matrix product 1226). With half the LDS reads left out the time
-// is the same, without the exponentials 530 us. Small calls are 10 us of launch, dependent loads and first bytes, and 2.2 us a listed block at 2 x 4096
+// tokens, 16 heads of 64, 64 of 516 blocks 598 us = 925 TFLOP/s (a large matrix product 1226). At 609 us, half the LDS reads left out changed
+// nothing, and leaving out the exponentials gave 530. Small calls are 10 us of launch, dependent loads and first bytes, and 2.2 us a listed block at 2 x 4096
 // tokens (985 TFLOP/s).
 #include <atomic>
 

@@ -41,7 +41,7 @@ template <class T> __device__ __forceinline__ void turn_pair(T& u, T& v, float c
 // A workgroup turns `tokens` tokens of one batch element. Cosine and sine of a (token, pair) are the same for every head: they are
 // formed once, in LDS, and the heads stream past. A thread's unit is VEC pairs of one head: two packets of VEC channels
 // (HALF) or one of 2 VEC (interleaved); behind a head's pairs come packets of VEC channels that are copied. Bound by the bytes: 2 x 4096
-// tokens, 32 heads of 64, bf16, 12.6 us = 5.3 TB/s (a large copy 5.2); with two or four units of a thread under way at a time 13 to 15.
+// tokens, 32 heads of 64, bf16, 13.2 us = 5.1 TB/s (a large copy 5.2); with two or four units of a thread under way at a time 15.0, 13.7.
 template <class T, int VEC, bool HALF>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, const T* x, const int32_t* __restrict__ pos, T* y) {
   extern __shared__ __attribute__((aligned(16))) float cs[];  // [token][pair][cos, sin]
@@ -143,7 +143,7 @@ __device__ __forceinline__ void sum_rows(const T* base, int64_t ld, int r0, int 
 
 // A workgroup forms the means of four neighbouring blocks of one (batch element, key head), one a wavefront: its lanes take the
 // packets of as many rows at a time as they cover. Bound by the bytes, and by how short its workgroups live: 2 x 4096 keys, 16 heads of 64,
-// bf16, 6.4 us for 16.8 MB, 2 x 20011 17.3 us for 67.6 MB (3.9 TB/s).
+// bf16, 6.3 us for 16.8 MB, 2 x 20011 17.3 us for 67.6 MB (3.9 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void block_means_kernel(const T* __restrict__ k, lc_strides ks, const int32_t* __restrict__ k_len,
                                                           double* __restrict__ means, int Tk, int Hkv, int d, int block, int nk,
@@ -197,7 +197,7 @@ __device__ __forceinline__ uint64_t order_of(double s) {
 // 8 / R wavefronts a group; then the scores, a lane a block, RPT groups at a time (so that a mean that is read serves RPT scores),
 // into LDS as ordered numbers; then a wavefront a group searches the keep-th largest of them bit by bit, HELD of them a lane in
 // registers and the rest in LDS, and writes what is not below it, by ascending block. What it takes: 2 x 20011 tokens, 313 blocks, 16 heads of 64
-// 36.5 us, of which pooling 43 % (67.6 MB of queries), scores 32 % (waits for L2), search 25 %; 2 x 4096, 64 blocks 11.4.
+// 36.3 us, of which pooling 43 % (67.6 MB of queries), scores 32 % (waits for L2), search 25 %; 2 x 4096, 64 blocks 11.2.
 template <class T, int R, int RPT, int HELD>
 __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T* __restrict__ q, const double* __restrict__ means,
                                                            int32_t* __restrict__ index) {
@@ -492,7 +492,7 @@ lc_status lc_op_rope(const lc_rope_table* t, const lc_rope_args* a, const void* 
   const int vec = half && bf && fits(8) ? 8 : (half || bf) && fits(4) ? 4 : !half && !bf && fits(2) ? 2 : 1;
   // Tokens a workgroup: some 1024 units, four a thread, so that the trigonometry is shared out and few workgroups start (32 heads of 64: 4
   // tokens 13.7 us, one 17.7; 16 heads: 8 tokens 29.5 us of 123 MB, one 53.6), as long as there are two for each compute unit (1000
-  // tokens: 5.1 us, with 8 a workgroup 6.6)
+  // tokens of 32 heads: one 5.3 us, 8 a workgroup 6.6)
   const int units = a->heads * (k.pairs / vec + k.rest / vec);
   k.tokens = 1;
   while (k.tokens < 64 && 2 * k.tokens * (int64_t)units <= 1024 && (int64_t)a->B * ((a->T + 2 * k.tokens - 1) / (2 * k.tokens)) >= 512) k.tokens *= 2;
