@@ -633,7 +633,7 @@ typedef struct lc_entry_args {
 } lc_entry_args;
 size_t lc_entry_packed_bytes(const lc_entry_args* args); /* host only; 0 if format or sizes are refused */
 /* Writes the entry [device, 16-byte aligned] of x; with y also y = base + what the entry now stands for, in the same pass (base NULL:
- * zeros; base may be y, and x may be base or y). lc_op_entry_unpack reads it back: y = base + values. */
+ * zeros; base may be y, and x, of the same type and row stride, base or y). lc_op_entry_unpack reads it back: y = base + values. */
 lc_status lc_op_entry_pack(const lc_entry_args* args, const void* x, void* entry, const void* base, void* y, void* stream);
 lc_status lc_op_entry_unpack(const lc_entry_args* args, const void* entry, const void* base, void* y, void* stream);
 

@@ -224,6 +224,8 @@ lc_status lc_op_entry_pack(const lc_entry_args* a, const void* x, void* entry, c
   if (y) {
     if (!is_dtype(a->y_dtype)) return bad(LC_ERR_ARG, "y_dtype must be LC_F32 or LC_BF16");
     if (a->y_ld < a->cols && a->rows > 1) return bad(LC_ERR_SHAPE, "y_ld must be at least cols");
+    if (x == y && (a->x_dtype != a->y_dtype || (a->x_ld != a->y_ld && a->rows > 1)))
+      return bad(LC_ERR_SHAPE, "in place, x and y have the same type and rows");
   }
   const int ydt = y ? a->y_dtype : LC_F32;
   const bool whole = a->cols % 4 == 0 && aligned_for4(x, a->x_ld, a->x_dtype) && (!y || aligned_for4(y, a->y_ld, ydt)) &&

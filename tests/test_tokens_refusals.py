@@ -172,6 +172,12 @@ def test_entries():
     assert lcb.lc_entry_packed_bytes(entry_args(format=7)) == 0 and lcb.lc_entry_packed_bytes(entry_args(rows=0)) == 0
 
 
+def test_entries_written_over_their_values_keep_rows_in_place():
+    """A thread's values go where other threads still read, unless rows and types are the same."""
+    for kw in (dict(y_ld=104), dict(x_ld=104), dict(y_dtype=lcb.LC_BF16), dict(x_dtype=lcb.LC_BF16)):
+        refused(2, "in place", lambda: lcb.lc_op_entry_pack(entry_args(**kw), P, P, None, P, None))
+
+
 def test_tensors_that_are_refused_before_the_library():
     """There is no CPU fallback, and shapes and types are told apart by name."""
     x = torch.zeros(1, 4, 2, 64)
