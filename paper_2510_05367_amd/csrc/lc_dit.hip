@@ -242,6 +242,7 @@ lc_status check_topt(lc_dit* c, const lc_dit_config& g, const lc_dit_options* op
   t->o = *opt;
   t->o.rope = nullptr;
   if (opt->entry_format < LC_ENTRY_PLAIN || opt->entry_format > LC_ENTRY_FP4) return tfail(c, LC_ERR_ARG, "entry_format must be one of LC_ENTRY_PLAIN .. LC_ENTRY_FP4");
+  if (entry_bytes(g, *t) == 0) return tfail(c, LC_ERR_SHAPE, "an entry holds less than 2^34 values");
   if (opt->keep < 0) return tfail(c, LC_ERR_ARG, "keep must not be negative");
   if (opt->keep > 0) {
     const lc_sparse_args a = sparse_args(g, *opt);

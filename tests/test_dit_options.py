@@ -53,6 +53,19 @@ def test_entries_take_what_their_codes_take(fmt, share):
         assert lcb.lc_dit_options_workspace_bytes(cfg, lcb.make_dit_options(entry=fmt), chunk) == lcb.lc_dit_workspace_bytes(cfg, chunk) - plain + 2 * packed
 
 
+@pytest.mark.parametrize("fmt", ["mxint8", "mxfp8", "mxfp4"])
+def test_entries_beyond_their_sizes_are_refused(fmt):
+    """2^24 tokens of 2048 channels are a stack's limits, and more values than an entry holds."""
+    cfg = lcb.make_dit_config(BIG, 0, 1)
+    cfg.B, cfg.T, cfg.D, cfg.heads, cfg.head_dim = 1, 1 << 24, 2048, 32, 64
+    assert lcb.lc_dit_entry_bytes(cfg) == 1 << 37
+    with pytest.raises(lcb.LcError, match="values") as e:
+        lcb.lc_dit_check_options(cfg, lcb.make_dit_options(entry=fmt))
+    assert e.value.status == 2 and lcb.lc_dit_options_workspace_bytes(cfg, lcb.make_dit_options(entry=fmt), 0) == 0
+    cfg.T = (1 << 23) - 1
+    lcb.lc_dit_check_options(cfg, lcb.make_dit_options(entry=fmt))
+
+
 def test_selection_takes_no_transposed_values():
     cfg = lcb.make_dit_config(BIG, 0, 1)
     R, D = BIG.B * BIG.T, BIG.D
