@@ -560,6 +560,7 @@ lc_status lc_op_block_attention(const lc_sparse_args* a, const void* q, const vo
   if (need > 0 && (uintptr_t)workspace % 16) return (lc_status)op_fail(LC_ERR_ARG, "workspace must be 16-byte aligned");
   BlockAttnArgs k_;
   k_.qs = a->q; k_.ks = a->k; k_.vs = a->v; k_.os = a->out;
+  if (a->Tk == 1) k_.ks.token = k_.vs.token = a->head_dim;  // (any stride says the same; this one puts rows that do not exist out of range)
   k_.index = index; k_.q_len = q_len; k_.k_len = k_len;
   k_.part = (float*)workspace;
   k_.scale = a->q_prescaled ? 1.f : attn_q_scale(a->head_dim);

@@ -286,6 +286,28 @@ def test_attention_memory_layouts(dtype, Tq, q_block):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("Tq", [2, 50, 100])
+def test_attention_of_one_key(dtype, Tq):
+    """The stride of an axis of one token says nothing (zero, here); the one value is the result, infinities too."""
+    rng = np.random.default_rng(17)
+    q, k, v = (gpu(rng.normal(size=(1, n, 2, 64)), dtype) for n in (Tq, 1, 1))
+    v[0, 0, 1, 5], v[0, 0, 0, 63] = float("inf"), -float("inf")
+    out, one, row = torch.full_like(q, 77.0), lcb.lc_strides(0, 0, 64), lcb.lc_strides(0, 128, 64)
+    a = lcb.lc_sparse_args(B=1, Tq=Tq, Tk=1, heads=2, kv_heads=2, head_dim=64, dtype=lcb.LC_BF16 if dtype == BF else lcb.LC_F32, block=64,
+                           q_block=128, keep=1, window=-1, q=row, k=one, v=one, out=row)
+    assert lcb.lc_block_attention_workspace(a) == 0
+    index = ints([[[[0]], [[0]]]])
+    lcb.lc_op_block_attention(a, q.data_ptr(), k.data_ptr(), v.data_ptr(), index.data_ptr(), None, None, out.data_ptr(), None, 0,
+                              torch.cuda.current_stream().cuda_stream)
+    # The one probability p (1, or next to it: its exponent is what a fused product leaves of a rounded one) is the denominator too,
+    # so a result is fl(fl(p v) fl(1 / p)): three roundings, less than (1 + 2^-24)^3 - 1 < 2^-22 of v in float, and nothing
+    # once it is rounded to bf16, where v lies.
+    want, some = v.expand(1, Tq, 2, 64), torch.isfinite(v).expand(1, Tq, 2, 64)
+    assert torch.equal(out[~some], want[~some])
+    assert torch.all((out[some].double() - want[some].double()).abs() <= (0.0 if dtype == BF else 2.0 ** -22) * want[some].double().abs())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Tq", [2, 50, 100])
 def test_lists_of_any_origin(dtype, Tq):
     """A list ends at its first entry that is no block with a key, or that does not ascend; blocks behind k_len have none."""
     rng = np.random.default_rng(12)
