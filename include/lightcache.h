@@ -531,8 +531,8 @@ lc_status lc_unet_cache_dev_peek(lc_unet* ctx, int dev_slot, const void** ptr /*
  *     axes in elements (channels lie next to each other): rows of packed q,k,v, heads in front of tokens and tensors that one
  *     batch element shares (stride 0, inputs only) are all of this form. Elements are of `dtype` (lc_dtype).
  *   - Lengths q_len, k_len [device, int32, B] or NULL: of batch element b only the first q_len[b] queries / k_len[b] keys
- *     exist (values are clamped to [0, Tq] / [0, Tk]). What lies behind is never read; rows of outputs behind q_len[b] are
- *     left as they were. */
+ *     exist (values are clamped to [0, Tq] / [0, Tk]). Keys and values behind are never read. Queries behind, up to Tq,
+ *     have to be memory that may be read, but what they hold goes into nothing; rows of outputs behind q_len[b] are left as they were. */
 typedef struct lc_strides { int64_t batch, token, head; } lc_strides;
 
 /* Rotary positions. The first rot_dim = axis_dim[0] + .. channels of a head are pairs (u, v), which a token at position p

@@ -106,7 +106,8 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
   const int most = min(a.Tq - row0, min(a.q_block - part * (128 / KS), 128 / KS));  // and how many there could be
 
   // ---- queries: B operand of S^T = K Q^T; packets beyond D and rows beyond the group are zeros. (Rows behind q_len may hold anything: a
-  // query's column of everything below is its own, and theirs are not stored.)
+  // query's column of everything below is its own, and theirs are not stored. Were the length waited for, 4 x 3 queries would take 10.2 us
+  // in place of 8.6, without lengths too.)
   const int qi = wid / KS * 32 + lq;
   Vec16<T> qf[STEPS];
 #pragma unroll
