@@ -186,6 +186,8 @@ struct SelectArgs {
   int Tq, Tk, H, Hkv, d, block, q_block, keep, sink, window, nq, nk, slices;
 };
 
+constexpr int kQM = 132;  // doubles from one group's means to the next in LDS: what four groups read at a time lies in different banks
+
 // Scores as unsigned numbers of the same order: 0 no block, 1 a score that is no number, all ones a block that is forced.
 __device__ __forceinline__ uint64_t order_of(double s) {
   const uint64_t u = (uint64_t)__double_as_longlong(s + 0.0);  // (-0 is 0)
@@ -194,17 +196,17 @@ __device__ __forceinline__ uint64_t order_of(double s) {
 }
 
 // A workgroup of eight wavefronts selects for R neighbouring groups of one (batch element, head). Means of the groups' queries first,
-// 8 / R wavefronts a group; then the scores, a lane a block, RPT groups at a time (so that a mean that is read serves RPT scores),
-// into LDS as ordered numbers; then a wavefront a group searches the keep-th largest of them bit by bit, HELD of them a lane in
-// registers and the rest in LDS, and writes what is not below it, by ascending block. What it takes: 2 x 20011 tokens, 313 blocks, 16 heads of 64
-// 36.3 us, of which pooling 43 % (67.6 MB of queries), scores 32 % (waits for L2), search 25 %; 2 x 4096, 64 blocks 11.2.
-template <class T, int R, int RPT, int HELD>
+// 8 / R wavefronts a group; then the scores, 16 blocks a wavefront at a time, into LDS as ordered numbers; then a wavefront a group
+// searches the keep-th largest of them bit by bit, HELD of them a lane in registers and the rest in LDS, and writes what is not below
+// it, by ascending block. Nearly half of the time goes into pooling the queries (2 x 20011 tokens, 313 blocks, 16 heads of 64 34.0 us, 67.6 MB), the rest
+// into scores and search; 2 x 4096 tokens, 64 blocks 9.8 us.
+template <class T, int R, int HELD>
 __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T* __restrict__ q, const double* __restrict__ means,
                                                            int32_t* __restrict__ index) {
-  constexpr int VEC = Vec16<T>::N, WPR = 8 / R, RS = R / RPT;
+  constexpr int VEC = Vec16<T>::N, WPR = 8 / R, G4 = (R + 3) / 4;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  double (*const qm)[128] = reinterpret_cast<double (*)[128]>(smem);      // [R][128]
-  uint64_t* const keys = reinterpret_cast<uint64_t*>(smem + R * 128 * 8);   // [R][nk]; before that the sums of eight wavefronts
+  double (*const qm)[kQM] = reinterpret_cast<double (*)[kQM]>(smem);      // [R][kQM]
+  uint64_t* const keys = reinterpret_cast<uint64_t*>(smem + R * kQM * 8);   // [R][nk]; before that the sums of eight wavefronts
   double* const part = reinterpret_cast<double*>(keys);
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   // (heads first: as above, and where they are a multiple of eight all groups of a head find its means in one XCD's L2)
@@ -235,41 +237,40 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
   }
   __syncthreads();
 
+  // Scores of 16 blocks at a time on the matrix cores: four 4 x 4 x 4 products side by side, whose rows are four groups and whose 16 columns
+  // are the blocks. (A lane a block and fused multiply-adds, whose every score reads its group's mean out of LDS, take 19.7 us in place of 14.4 at
+  // 2 x 8192 tokens.)
   const double* const mb = means + ((int64_t)b * a.Hkv + h / (a.H / a.Hkv)) * d * nk;
   {
-    const int rs = (wid % RS) * RPT;
-    for (int jc = wid / RS; jc * 64 < nk; jc += 8 / RS) {
-      const int j = jc * 64 + lane;
-      double s[RPT];
+    const int kq = lane >> 4;
+    const double* const qa = &qm[(lane & 3) % R][kq];
+    for (int j = wid * 16 + (lane & 15); j - (lane & 15) < live; j += 8 * 16) {
+      const double* const mj = mb + (int64_t)kq * nk + min(j, nk - 1);  // (behind the last block it stands in: nothing of it is kept)
+      double s[G4];
 #pragma unroll
-      for (int r = 0; r < RPT; ++r) s[r] = 0.0;
-      if (j < live) {
-        auto batch = [&](int c0, auto n_c) {
-          constexpr int N = decltype(n_c)::value;
-          double m[N];
+      for (int u = 0; u < G4; ++u) s[u] = 0.0;
+      auto batch = [&](int c0, auto n_c) {
+        constexpr int N = decltype(n_c)::value;
+        double m[N];
 #pragma unroll
-          for (int c = 0; c < N; ++c) m[c] = mb[(int64_t)(c0 + c) * nk + j];
-          __builtin_amdgcn_sched_barrier(0);
+        for (int c = 0; c < N; ++c) m[c] = mj[(int64_t)(c0 + 4 * c) * nk];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int c = 0; c < N; ++c)
+        for (int c = 0; c < N; ++c)
 #pragma unroll
-            for (int r = 0; r < RPT; ++r) s[r] = fma(qm[rs + r][c0 + c], m[c], s[r]);
-        };
-        // Means under way at a time: few groups wait for them (2 x 4096 tokens: 32 at a time 11.5 us, eight 13.1), many would have
-        // 104 registers with 32 and two workgroups a compute unit in place of three (2 x 20011: 48 us, with eight 37)
-        int c0 = 0;
-        if (RPT <= 2)
-          for (; c0 + 32 <= d; c0 += 32) batch(c0, std::integral_constant<int, 32>{});
-        for (; c0 < d; c0 += 8) batch(c0, std::integral_constant<int, 8>{});
-      }
-      if (j < nk) {
+          for (int u = 0; u < G4; ++u)
+            s[u] = __builtin_amdgcn_mfma_f64_4x4x4f64(qa[u * 4 * kQM + c0 + 4 * c], m[c], s[u], 0, 0, 0);
+      };
+      int c0 = 0;
+      for (; c0 + 64 <= d; c0 += 64) batch(c0, std::integral_constant<int, 16>{});
+      for (; c0 < d; c0 += 8) batch(c0, std::integral_constant<int, 2>{});
 #pragma unroll
-        for (int r = 0; r < RPT; ++r) {
-          const int64_t p0 = a.q_pos0 + (int64_t)(g0 + rs + r) * a.q_block, p1 = min(p0 + a.q_block, a.q_pos0 + a.Tq) - 1;
-          const bool near = a.window >= 0 && (int64_t)(j - a.window) * a.block <= p1 &&
-                            (int64_t)(j + a.window + 1) * a.block > p0;  // (both say what a floor would, below zero too)
-          keys[(rs + r) * nk + j] = j >= live ? 0 : j < a.sink || near ? ~0ull : order_of(s[r]);
-        }
+      for (int u = 0; u < G4; ++u) {
+        const int r = u * 4 + kq;
+        const int64_t p0 = a.q_pos0 + (int64_t)(g0 + r) * a.q_block, p1 = min(p0 + a.q_block, a.q_pos0 + a.Tq) - 1;
+        const bool near = a.window >= 0 && (int64_t)(j - a.window) * a.block <= p1 &&
+                          (int64_t)(j + a.window + 1) * a.block > p0;  // (both say what a floor would, below zero too)
+        if (r < R && j < live) keys[r * nk + j] = j < a.sink || near ? ~0ull : order_of(s[u]);
       }
     }
   }
@@ -550,32 +551,30 @@ lc_status lc_op_block_select(const lc_sparse_args* a, const void* q, const doubl
   k.qs = a->q; k.q_len = q_len; k.k_len = k_len; k.q_pos0 = a->q_pos0;
   k.Tq = a->Tq; k.Tk = a->Tk; k.H = a->heads; k.Hkv = a->kv_heads; k.d = a->head_dim; k.block = a->block; k.q_block = a->q_block;
   k.keep = a->keep; k.sink = a->sink; k.window = a->window > 1 << 16 ? 1 << 16 : a->window; k.nq = lc_sparse_groups(a); k.nk = lc_sparse_blocks(a);
-  // Groups a workgroup: as many as share the means best while there are two workgroups for each compute unit, and while the
-  // scores' numbers fit into 64 KiB (us with 1, 2, 4, 8 groups: 2 x 4096 tokens, 32 groups a head 15.1, 11.4, 12.1, 13.6; 2 x 8192 -, 24.5, 19.4, 17.8;
-  // 2 x 20011 -, -, 48.4, 37.0)
+  // Groups a workgroup: as many as share the means best while there is a workgroup for each compute unit, and while the
+  // scores' numbers fit into 64 KiB (us with 256 workgroups at least, and with 512: 2 x 4096 tokens 9.8 and 10.2, 1 x 4096 8.6 and 9.7, 2 x 8192 14.0 and 14.4,
+  // 1 x 12000 15.1 and 16.9; with 128: 10.7, 8.7, 13.7, 15.5)
   const int64_t bh = (int64_t)a->B * a->heads;
   int R = 8;
-  while (R > 1 && (bh * ((k.nq + R - 1) / R) < 512 || R * (k.nk + 128) > 8192)) R /= 2;
+  while (R > 1 && (bh * ((k.nq + R - 1) / R) < 256 || R * (k.nk + kQM) > 8192)) R /= 2;
   k.slices = (k.nq + R - 1) / R;
   const int64_t blocks = bh * k.slices;
   if (blocks > (int64_t)1 << 22) return bad(LC_ERR_SHAPE, "too many groups of queries");
   const size_t sums = (size_t)8 * 64 * (a->dtype == LC_BF16 ? 8 : 4) * 8, nums = (size_t)R * k.nk * 8;
-  const size_t lds = (size_t)R * 128 * 8 + (sums > nums ? sums : nums);
-#define LC_RUN(T, R_, P_, N_)                                                                                                      \
+  const size_t lds = (size_t)R * kQM * 8 + (sums > nums ? sums : nums);
+#define LC_RUN(T, R_, N_)                                                                                                          \
   do {                                                                                                                             \
-    const hipError_t e = lds <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)block_select_kernel<T, R_, P_, N_>,          \
+    const hipError_t e = lds <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)block_select_kernel<T, R_, N_>,              \
                                                                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);    \
     if (e != hipSuccess) return (lc_status)op_fail(LC_ERR_HIP, "block_select: %s", hipGetErrorString(e));                          \
-    block_select_kernel<T, R_, P_, N_><<<(unsigned)blocks, 512, lds, (hipStream_t)stream>>>(k, (const T*)q, means, index);         \
+    block_select_kernel<T, R_, N_><<<(unsigned)blocks, 512, lds, (hipStream_t)stream>>>(k, (const T*)q, means, index);             \
   } while (0)
-#define LC_GO(R_, P_, N_) do { if (a->dtype == LC_BF16) LC_RUN(bf16_t, R_, P_, N_); else LC_RUN(float, R_, P_, N_); } while (0)
-  // Groups a lane scores at once: what this is bound by is L2, which every means goes through once for them all (2 x 20011 tokens, 313
-  // blocks: 8 groups 36.5 us, 4 groups 39.3), but not so many that few wavefronts have blocks
+#define LC_GO(R_, N_) do { if (a->dtype == LC_BF16) LC_RUN(bf16_t, R_, N_); else LC_RUN(float, R_, N_); } while (0)
+  // (as many held as there are, where that is few: 313 blocks 35.3 us with five, 36.9 with eight)
+#define LC_HELD(R_) do { if (chunks > 5) LC_GO(R_, 8); else if (chunks > 2) LC_GO(R_, 5); else if (chunks > 1) LC_GO(R_, 2); else LC_GO(R_, 1); } while (0)
   const int chunks = (k.nk + 63) / 64;
-  if (R == 8) { if (chunks >= 4) LC_GO(8, 8, 8); else if (chunks >= 2) LC_GO(8, 2, 3); else LC_GO(8, 1, 1); }
-  else if (R == 4) { if (chunks >= 8) LC_GO(4, 4, 8); else if (chunks >= 4) LC_GO(4, 2, 8); else LC_GO(4, 1, 3); }
-  else if (R == 2) { if (chunks >= 8) LC_GO(2, 2, 8); else if (chunks >= 2) LC_GO(2, 1, 8); else LC_GO(2, 1, 1); }
-  else { if (chunks >= 2) LC_GO(1, 1, 8); else LC_GO(1, 1, 1); }
+  if (R == 8) LC_HELD(8); else if (R == 4) LC_HELD(4); else if (R == 2) LC_HELD(2); else LC_HELD(1);
+#undef LC_HELD
 #undef LC_GO
 #undef LC_RUN
   return launched("block_select");
