@@ -198,6 +198,23 @@ def test_selection_ties_nan_and_long_lists():
     assert got[0, 0, 0].tolist() == list(range(0, 8192, 1000))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("nk", [40, 100, 300, 500])
+def test_selection_by_few_and_many_groups(dtype, nk):
+    """Eight, four, two groups or one a workgroup, and more or fewer blocks than are held in registers, list alike; a block whose mean is
+    no number changes no other's place."""
+    rng = np.random.default_rng(nk)
+    H, d, keep = 32, 16, 7
+    k, q = gpu(clusters(rng, 1, nk * 64, 4, d), dtype), gpu(rng.normal(size=(1, 64, H, d)), dtype)
+    k[0, 17 * 64 + 5, 1, 3], k[0, -1, 2, 0] = NAN, float("inf")
+    means = tokens.block_means(k)
+    got = tokens.block_select(q, means, nk * 64, keep, q_block=1, sink=1)
+    want = tko.block_select(f64(q), tko.block_means(f64(k), 64), nk * 64, keep, 64, 1, sink=1)
+    assert np.array_equal(got.cpu().numpy(), want)
+    for n in (4, 16, 32, 33):
+        assert torch.equal(tokens.block_select(q[:, :n], means, nk * 64, keep, q_block=1, sink=1), got[:, :, :n]), n
+
+
 def test_means_of_a_growing_cache():
     rng = np.random.default_rng(9)
     k = gpu(rng.normal(size=(2, 1000, 3, 32)), BF)
