@@ -590,7 +590,7 @@ typedef struct lc_sparse_args {
   int32_t B, Tq, Tk, heads, kv_heads, head_dim, dtype;
   int32_t block, q_block, keep;
   int32_t sink, window;    /* selection: blocks that every list holds: the first `sink` ones, and those that hold or are at most
-                              `window` away from a block that holds the positions of the group's queries (window < 0: none) */
+                              `window` away from a block that holds the positions of the group's existing queries (window < 0: none) */
   int64_t q_pos0;          /* position of the first query among the keys */
   int32_t q_prescaled;     /* attention: 1 = q holds Q * log2(e) / sqrt(head_dim), as the projections of the steps write it */
   lc_strides q, k, v, out;

@@ -67,7 +67,7 @@ def block_select(q, means, Tk, keep, block, q_block, sink=0, window=-1, q_pos0=0
             for g in range(-(-ql // q_block)):
                 mean = q[b, g * q_block:min(ql, (g + 1) * q_block), h].astype(np.float64).mean(axis=0)
                 p0 = q_pos0 + g * q_block
-                p1 = q_pos0 + min(Tq, (g + 1) * q_block) - 1
+                p1 = q_pos0 + min(ql, (g + 1) * q_block) - 1
                 ranked = []
                 for j in range(-(-kl // block)):
                     s = float(mean @ means[b, h * Hkv // H, :, j])

@@ -267,7 +267,7 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
 #pragma unroll
       for (int u = 0; u < G4; ++u) {
         const int r = u * 4 + kq;
-        const int64_t p0 = a.q_pos0 + (int64_t)(g0 + r) * a.q_block, p1 = min(p0 + a.q_block, a.q_pos0 + a.Tq) - 1;
+        const int64_t p0 = a.q_pos0 + (int64_t)(g0 + r) * a.q_block, p1 = min(p0 + a.q_block, a.q_pos0 + qlen) - 1;  // (of queries that exist)
         const bool near = a.window >= 0 && (int64_t)(j - a.window) * a.block <= p1 &&
                           (int64_t)(j + a.window + 1) * a.block > p0;  // (both say what a floor would, below zero too)
         if (r < R && j < live) keys[r * nk + j] = j < a.sink || near ? ~0ull : order_of(s[u]);

@@ -1,0 +1,28 @@
+"""The operators of long videos where sequences, lists, number ranges and launches end, against their float64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tokens_oracle as tko
+from paper_2510_05367_amd import tokens
+from tests.test_gpu_tokens import BF, F32, NAN, clusters, f64, gpu, ints
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- selection -------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_forced_blocks_are_those_of_queries_that_exist(dtype):
+    """Keys reach beyond the queries: a short sequence's lists are those of the call that is not padded."""
+    rng = np.random.default_rng(21)
+    B, Tq, Tk, H, d, keep = 4, 300, 1000, 4, 32, 3
+    k, q = gpu(clusters(rng, B, Tk, 2, d), dtype), gpu(clusters(rng, B, Tq, H, d), dtype)
+    q_len = [1, 129, 300, 64]
+    means, ref = tokens.block_means(k), tko.block_means(f64(k), 64)
+    for q_block, window, pos0 in ((128, 0, 0), (100, 1, 40), (128, 2, 500), (7, 0, 63), (128, 0, -100)):
+        kw = dict(q_block=q_block, window=window, q_pos0=pos0)
+        got = tokens.block_select(q, means, Tk, keep, q_len=ints(q_len), **kw)
+        assert np.array_equal(got.cpu().numpy(), tko.block_select(f64(q), ref, Tk, keep, 64, q_len=q_len, **kw)), kw
+        for b, n in enumerate(q_len):
+            alone = tokens.block_select(q[b:b + 1, :n], means[b:b + 1].contiguous(), Tk, keep, **kw)
+            assert torch.equal(alone[0], got[b, :, :alone.shape[2]]), (kw, b)
