@@ -268,8 +268,8 @@ __global__ __launch_bounds__(512) void block_select_kernel(SelectArgs a, const T
       for (int u = 0; u < G4; ++u) {
         const int r = u * 4 + kq;
         const int64_t p0 = a.q_pos0 + (int64_t)(g0 + r) * a.q_block, p1 = min(p0 + a.q_block, a.q_pos0 + qlen) - 1;  // (of queries that exist)
-        const bool near = a.window >= 0 && (int64_t)(j - a.window) * a.block <= p1 &&
-                          (int64_t)(j + a.window + 1) * a.block > p0;  // (both say what a floor would, below zero too)
+        const bool near = a.window >= 0 && ((int64_t)j - a.window) * a.block <= p1 &&
+                          ((int64_t)j + a.window + 1) * a.block > p0;  // (both say what a floor would, below zero too)
         if (r < R && j < live) keys[r * nk + j] = j < a.sink || near ? ~0ull : order_of(s[u]);
       }
     }
@@ -550,7 +550,7 @@ lc_status lc_op_block_select(const lc_sparse_args* a, const void* q, const doubl
   SelectArgs k;
   k.qs = a->q; k.q_len = q_len; k.k_len = k_len; k.q_pos0 = a->q_pos0;
   k.Tq = a->Tq; k.Tk = a->Tk; k.H = a->heads; k.Hkv = a->kv_heads; k.d = a->head_dim; k.block = a->block; k.q_block = a->q_block;
-  k.keep = a->keep; k.sink = a->sink; k.window = a->window > 1 << 16 ? 1 << 16 : a->window; k.nq = lc_sparse_groups(a); k.nk = lc_sparse_blocks(a);
+  k.keep = a->keep; k.sink = a->sink; k.window = a->window; k.nq = lc_sparse_groups(a); k.nk = lc_sparse_blocks(a);
   // Groups a workgroup: as many as share the means best while there is a workgroup for each compute unit, and while the
   // scores' numbers fit into 64 KiB (us with 256 workgroups at least, and with 512: 2 x 4096 tokens 9.8 and 10.2, 1 x 4096 8.6 and 9.7, 2 x 8192 14.0 and 14.4,
   // 1 x 12000 15.1 and 16.9; with 128: 10.7, 8.7, 13.7, 15.5)

@@ -26,3 +26,16 @@ def test_forced_blocks_are_those_of_queries_that_exist(dtype):
         for b, n in enumerate(q_len):
             alone = tokens.block_select(q[b:b + 1, :n], means[b:b + 1].contiguous(), Tk, keep, **kw)
             assert torch.equal(alone[0], got[b, :, :alone.shape[2]]), (kw, b)
+
+
+def test_windows_of_any_width():
+    """Positions may lie as far from the keys as a window is wide."""
+    rng = np.random.default_rng(22)
+    Tk, block = 64 * 12, 64
+    k, q = gpu(rng.normal(size=(1, Tk, 2, 16)), F32), gpu(rng.normal(size=(1, 5, 2, 16)), F32)
+    means, ref = tokens.block_means(k), tko.block_means(f64(k), block)
+    most = 2 ** 31 - 1
+    for at, window in ((70000, 69995), (70000, 69990), (-70000, 70003), (2 ** 31, most), (-(2 ** 31), most), (0, most), (2 ** 34 - 2, most), (7, 65536)):
+        for keep in (2, 9):
+            got = tokens.block_select(q, means, Tk, keep, q_block=2, window=window, q_pos0=at * block)
+            assert np.array_equal(got.cpu().numpy(), tko.block_select(f64(q), ref, Tk, keep, block, 2, 0, window, at * block)), (at, window, keep)
