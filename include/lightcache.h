@@ -618,8 +618,9 @@ lc_status lc_op_block_attention(const lc_sparse_args* args, const void* q, const
                                 void* stream);
 
 /* Quantised cache entries. An entry holds rows of `cols` values in groups of 32 (the last of a row may be shorter) that share a
- * scale 2^e: e is the least integer, at least -127, with max |x| <= M 2^e, so that nothing saturates, and a value is stored as the code
- * nearest to x 2^-e (ties to even):
+ * scale 2^e: e is the least integer, at least -127, with max |x| <= M 2^e, and a value is stored as the code nearest to x 2^-e (ties
+ * to even) of those that stand for a float: nothing saturates but values within a step below 2^128, which fall to the largest
+ * code whose value is below that, and what an entry stands for stays as it is when it is packed again.
  *   LC_ENTRY_INT8  integers, M = 127        LC_ENTRY_FP8  e4m3, M = 448        LC_ENTRY_FP4  e2m1, M = 6 (the first of two in the low bits)
  * Scales are bytes e + 127. A group that holds an infinity or a NaN is marked by the byte 255 and reads back as NaN. Codes
  * come first, rows of ceil(cols / 32) * 32 (zeros behind the last column), then the scale bytes, ceil(cols / 32) a row. */

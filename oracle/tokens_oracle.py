@@ -122,8 +122,12 @@ def magnitudes(fmt):
     return np.array(small + [(1 + f / 8) * 2.0 ** (e - 7) for e in range(1, 16) for f in range(8)][:-1])
 
 
+FLOAT_MAX = (2.0 - 2.0 ** -23) * 2.0 ** 127
+
+
 def entry(x, fmt):
-    """x [rows, cols] float32 -> (values the entry stands for, scale exponents [rows, groups]; exponent 128 marks no number)."""
+    """x [rows, cols] float32 -> (values the entry stands for, scale exponents [rows, groups]; exponent 128 marks no number). A code is
+    the nearest one whose value a float holds."""
     rows, cols = x.shape
     steps = magnitudes(fmt)
     top = steps[-1]
@@ -138,10 +142,11 @@ def entry(x, fmt):
             while np.abs(v).max(initial=0.0) > top * 2.0 ** e:
                 e += 1
             exps[r, g] = e
+            held = steps[steps * 2.0 ** e <= FLOAT_MAX]
             for i, a in enumerate(np.abs(v) / 2.0 ** e):
-                up = int(np.searchsorted(steps, a))
-                if up == 0:
-                    code = 0
+                up = int(np.searchsorted(held, a))
+                if up == 0 or up == len(held):
+                    code = min(up, len(held) - 1)
                 else:
                     hi, lo = steps[up] - a, a - steps[up - 1]
                     code = up if hi < lo or (hi == lo and up % 2 == 0) else up - 1

@@ -16,10 +16,13 @@ __device__ __forceinline__ float scale_down(int byte) {  // 2^-e; byte <= 254
   return __uint_as_float(byte == 254 ? 0x00400000u : (uint32_t)(254 - byte) << 23);
 }
 
-// Per format: codes of N neighbouring values in a packet of N * kBits / 8 bytes.
+// Per format: codes of N neighbouring values in a packet of N * kBits / 8 bytes. kLast is the largest magnitude below 2^(kTopExp): in
+// groups of the largest scale that a float can ask for, 2^(128 - kTopExp), the codes from there on stand for 2^128 and more, which
+// no float holds.
 template <int F> struct Code;
 template <> struct Code<LC_ENTRY_INT8> {
   static constexpr int kBits = 8, kTopExp = 6;
+  static constexpr float kLast = 63.f;
   static constexpr uint32_t kTopFrac = 0x7e0000u;  // 127 = 1.984375 * 2^6
   static __device__ __forceinline__ uint32_t pack4(const float (&u)[4]) {
     uint32_t w = 0;
@@ -34,6 +37,7 @@ template <> struct Code<LC_ENTRY_INT8> {
 };
 template <> struct Code<LC_ENTRY_FP8> {
   static constexpr int kBits = 8, kTopExp = 8;
+  static constexpr float kLast = 240.f;
   static constexpr uint32_t kTopFrac = 0x600000u;  // 448 = 1.75 * 2^8
   static __device__ __forceinline__ uint32_t pack4(const float (&u)[4]) {
     int w = 0;
@@ -52,6 +56,7 @@ template <> struct Code<LC_ENTRY_FP8> {
 };
 template <> struct Code<LC_ENTRY_FP4> {
   static constexpr int kBits = 4, kTopExp = 2;
+  static constexpr float kLast = 3.f;
   static constexpr uint32_t kTopFrac = 0x400000u;  // 6 = 1.5 * 2^2
   static __device__ __forceinline__ uint32_t pack4(const float (&u)[4]) {
     uint32_t w = 0;
@@ -135,9 +140,10 @@ __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_l
   const bool number = top < 0x7f800000u;
   const int byte = number ? max((int)(top >> 23) - C::kTopExp + ((top & 0x7fffffu) > C::kTopFrac), 0) : 255;
   const float down = number ? scale_down(byte) : 0.f;
+  const float most = byte == 255 - C::kTopExp ? C::kLast : INFINITY;  // (a finite value stays one)
   float u[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) u[e] = number ? v[e] * down : 0.f;
+  for (int e = 0; e < 4; ++e) u[e] = number ? fminf(fmaxf(v[e] * down, -most), most) : 0.f;
   const uint32_t w = C::pack4(u);
   if (!live) return;
   put_codes<F>(codes + (int64_t)i * (C::kBits / 2), w);

@@ -39,3 +39,25 @@ def test_windows_of_any_width():
         for keep in (2, 9):
             got = tokens.block_select(q, means, Tk, keep, q_block=2, window=window, q_pos0=at * block)
             assert np.array_equal(got.cpu().numpy(), tko.block_select(f64(q), ref, Tk, keep, block, 2, 0, window, at * block)), (at, window, keep)
+
+
+# ---- entries ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", ["mxint8", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_finite_entries_stay_finite_and_as_they_are(fmt, dtype):
+    """Values at the top of the range, beside others of every size: what they are held as is finite, and is packed to itself."""
+    rng = np.random.default_rng(23)
+    big = float(torch.finfo(dtype).max)
+    x = np.exp2(rng.uniform(100, 128, size=(64, 96))) * rng.choice([-1.0, 1.0], size=(64, 96))
+    x = np.clip(x, -big, big)
+    x[::2, ::32], x[1::4, 5::32] = big, -big * (1 - 2.0 ** -6)
+    t = torch.from_numpy(x).to("cuda", dtype)
+    ref, exps = tko.entry(f64(t), fmt)
+    y = torch.empty(64, 96, device="cuda")
+    entry = tokens.entry_pack(t, fmt, out=y)
+    assert np.array_equal(entry[-64 * 3:].cpu().numpy().reshape(64, 3), exps + 127)
+    assert bool(torch.isfinite(y).all()) and np.array_equal(f64(y), ref) and torch.equal(tokens.entry_unpack(entry, 64, 96, fmt), y)
+    small = tokens.entry_unpack(entry, 64, 96, fmt, dtype=BF)
+    assert np.array_equal(f64(small), ref)  # (codes have at most 7 bits: bf16 holds them too)
+    for again in (y, small):
+        assert torch.equal(tokens.entry_unpack(tokens.entry_pack(again, fmt), 64, 96, fmt), y)
