@@ -585,7 +585,7 @@ lc_status lc_op_rope(const lc_rope_table* table /* [host] */, const lc_rope_args
  * head h / (heads / kv_heads).
  * Requirements (else LC_ERR_SHAPE): sizes > 0; heads a multiple of kv_heads; head_dim in {8, 16, 32, 40, 64, 128}; block a
  * multiple of 64, at most 2^20; 1 <= q_block <= 128; keep <= 65536; Tk <= 2^30; at most 8192 blocks; strides and pointers of q, k, v and out such that every
- * head's row is 16-byte aligned; 64 token strides of k and v within 2^30 bytes. */
+ * head's row is 16-byte aligned; attention to more than one key: token strides of k and v at least head_dim, 64 of them within 2^30 bytes. */
 typedef struct lc_sparse_args {
   int32_t B, Tq, Tk, heads, kv_heads, head_dim, dtype;
   int32_t block, q_block, keep;

@@ -482,8 +482,10 @@ int check_attention(const lc_sparse_args* a) {
   int s = check_sparse_args(a);
   if (s != LC_OK) return s;
   const int64_t es = (int64_t)dtype_size(a->dtype), most = ((int64_t)1 << 30) / 64 / es;
-  if (a->k.token > most || a->v.token > most || a->k.token < 0 || a->v.token < 0) return op_fail(LC_ERR_SHAPE, "64 token strides of k and v must be within 2^30 bytes");
-  if (a->Tk > 1 && (a->k.token < a->head_dim || a->v.token < a->head_dim)) return op_fail(LC_ERR_SHAPE, "the rows of k and of v must not overlap");
+  if (a->Tk > 1) {  // (the token stride of one key says nothing)
+    if (a->k.token > most || a->v.token > most || a->k.token < 0 || a->v.token < 0) return op_fail(LC_ERR_SHAPE, "64 token strides of k and v must be within 2^30 bytes");
+    if (a->k.token < a->head_dim || a->v.token < a->head_dim) return op_fail(LC_ERR_SHAPE, "the rows of k and of v must not overlap");
+  }
   if (!strides_apart(a->out, a->B, a->Tq, a->heads)) return op_fail(LC_ERR_SHAPE, "the rows of out must not overlap");
   const int64_t groups = (int64_t)a->B * a->heads * lc_sparse_groups(a);
   if (groups > (int64_t)1 << 23) return op_fail(LC_ERR_SHAPE, "too many groups of queries");

@@ -41,6 +41,26 @@ def test_windows_of_any_width():
             assert np.array_equal(got.cpu().numpy(), tko.block_select(f64(q), ref, Tk, keep, block, 2, 0, window, at * block)), (at, window, keep)
 
 
+# ---- attention over the lists ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_first_key_of_a_cache_with_heads_in_front(dtype):
+    """One key of a long cache whose heads lie in front of its tokens: its rows are a whole head apart."""
+    rng = np.random.default_rng(24)
+    B, H, T, d = 2, 16, 16384, 64
+    k, v = (torch.full((B, H, T, d), NAN, dtype=dtype, device="cuda") for _ in range(2))
+    k[:, :, :2], v[:, :, :2] = gpu(rng.normal(size=(B, H, 2, d)), dtype), gpu(rng.normal(size=(B, H, 2, d)), dtype)
+    index = torch.zeros(B, H, 1, 1, dtype=torch.int32, device="cuda")
+    for Tq in (1, 40):
+        q = gpu(rng.normal(size=(B, Tq, H, d)), dtype)
+        for n in (1, 2):
+            kn, vn = (t[:, :, :n].transpose(1, 2) for t in (k, v))
+            got = tokens.block_attention(q, kn, vn, index)
+            assert torch.equal(got, tokens.block_attention(q, kn.contiguous(), vn.contiguous(), index)), (Tq, n)
+            means = tokens.block_means(kn)
+            assert torch.equal(means, tokens.block_means(kn.contiguous()))
+            assert torch.equal(tokens.block_select(q, means, n, 1), index)
+
+
 # ---- entries ---------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("fmt", ["mxint8", "mxfp8", "mxfp4"])
 @pytest.mark.parametrize("dtype", [F32, BF])
