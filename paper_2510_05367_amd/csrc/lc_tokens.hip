@@ -493,9 +493,10 @@ lc_status lc_op_rope(const lc_rope_table* t, const lc_rope_args* a, const void* 
   const int vec = half && bf && fits(8) ? 8 : (half || bf) && fits(4) ? 4 : !half && !bf && fits(2) ? 2 : 1;
   // Tokens a workgroup: some 1024 units, four a thread, so that the trigonometry is shared out and few workgroups start (32 heads of 64: 4
   // tokens 13.7 us, one 17.7; 16 heads: 8 tokens 29.5 us of 123 MB, one 53.6), as long as there are two for each compute unit (1000
-  // tokens of 32 heads: one 5.3 us, 8 a workgroup 6.6)
+  // tokens of 32 heads: one 5.3 us, 8 a workgroup 6.6). A launch counts its threads in 32 bits: 2^24 tokens and more are two at least.
   const int units = a->heads * (k.pairs / vec + k.rest / vec);
   k.tokens = 1;
+  while ((a->T + k.tokens - 1) / k.tokens >= 1 << 24) k.tokens *= 2;
   while (k.tokens < 64 && 2 * k.tokens * (int64_t)units <= 1024 && (int64_t)a->B * ((a->T + 2 * k.tokens - 1) / (2 * k.tokens)) >= 512) k.tokens *= 2;
   const dim3 grid((unsigned)((a->T + k.tokens - 1) / k.tokens), (unsigned)a->B);
   const size_t lds = (size_t)k.tokens * k.pairs * 8;

@@ -10,6 +10,22 @@ from tests.test_gpu_tokens import BF, F32, NAN, clusters, f64, gpu, ints
 pytestmark = pytest.mark.gpu
 
 
+# ---- rotary positions ------------------------------------------------------------------------------------------------
+def test_rope_of_2_to_24_tokens():
+    """As many tokens as a launch has workgroups of one: 635 units each (a pair and 126 channels that are copied, of five heads)."""
+    rng = np.random.default_rng(20)
+    T, H, d, ends = 1 << 24, 5, 128, 9
+    t = tokens.make_rope(d, axes=(2,))
+    row = gpu(rng.normal(size=(1, 1, H, d)), BF)
+    y = torch.zeros(1, T, H, d, dtype=BF, device="cuda")  # 21 GB
+    tokens.rope(row.expand(1, T, H, d), t, start=3, out=y)
+    for at in (0, T // 2 - 5, T - ends):
+        assert torch.equal(y[:, at:at + ends], tokens.rope(row.expand(1, ends, H, d).contiguous(), t, start=3 + at)), at
+    assert torch.equal(y[0, :, :, 2:].amax(0), row[0, 0, :, 2:]) and torch.equal(y[0, :, :, 2:].amin(0), row[0, 0, :, 2:])
+    del y
+    torch.cuda.empty_cache()
+
+
 # ---- selection -------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_forced_blocks_are_those_of_queries_that_exist(dtype):
