@@ -552,7 +552,7 @@ typedef struct lc_rope_config {
   int32_t head_dim, axes;  /* 2 .. 128; 1 .. 3 */
   int32_t axis_dim[3];     /* even, > 0 for the first `axes` of them; their sum at most head_dim */
   int32_t layout, scaling, orig_len; /* orig_len: LC_ROPE_PARTS only */
-  double base, factor;     /* base > 1; factor > 0 */
+  double base, factor;     /* base > 1; factor > 0, such that the scaled base is a positive finite number and every w at most 2^64 */
   double beta_fast, beta_slow; /* LC_ROPE_PARTS only, beta_fast > beta_slow (32 and 1 are usual) */
 } lc_rope_config;
 /* What lc_rope_make works out once for a model; plain data, copied by the calls that take it. */

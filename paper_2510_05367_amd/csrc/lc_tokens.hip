@@ -422,11 +422,13 @@ lc_status lc_rope_make(const lc_rope_config* g, lc_rope_table* out) {
   t.head_dim = g->head_dim; t.rot_dim = rot; t.axes = g->axes; t.layout = g->layout;
   t.amplitude = g->scaling == LC_ROPE_PARTS && g->factor > 1.0 ? 0.1 * std::log(g->factor) + 1.0 : 1.0;
   const double two_pi = 6.283185307179586476925286766559;
+  const double kFastest = 18446744073709551616.0;  // (such angles have long lost their precision, and end in infinities)
   int n = 0;
   for (int a = 0; a < g->axes; ++a) {
     const int D = g->axis_dim[a];
     t.axis_dim[a] = D;
     const double base = g->scaling == LC_ROPE_BASE && D > 2 ? g->base * std::pow(g->factor, (double)D / (D - 2)) : g->base;
+    if (!(base > 0.0) || !std::isfinite(base)) return bad(LC_ERR_SHAPE, "factor takes the base out of the range of 64 bits");
     for (int i = 0; i < D / 2; ++i) {
       double w = std::pow(base, -2.0 * i / D);
       if (g->scaling == LC_ROPE_LINEAR) w /= g->factor;
@@ -435,6 +437,7 @@ lc_status lc_rope_make(const lc_rope_config* g, lc_rope_table* out) {
         keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
         w = w * (keep + (1.0 - keep) / g->factor);
       }
+      if (!(w <= kFastest)) return bad(LC_ERR_SHAPE, "factor makes a pair turn more than 2^64 radians a position");
       t.turns[n++] = w / two_pi;
     }
   }
