@@ -177,7 +177,8 @@ __global__ __launch_bounds__(256, 2) void block_attn_kernel(BlockAttnArgs a, con
   };
   // The requests are written out, so that the compiler does not take the transposing reads below to depend on all of them and
   // waits for none: barrier_keep says when a stage is there. (No register is loaded. The wait states in front are what a load needs behind
-  // vector instructions that wrote its scalar operands.)
+  // vector instructions that wrote its scalar operands. m0, where the load finds its place in LDS, is reserved: the compiler warns of it in a clobber
+  // list and uses it for nothing else here, which a test of the compiled code holds it to.)
   auto issue = [&](int st, int key0) {
 #ifdef __HIP_DEVICE_COMPILE__
     const int keys = min(64, TK - key0);
