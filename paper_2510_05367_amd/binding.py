@@ -134,6 +134,13 @@ LC_ROPE_MAX_PAIRS = 64
 LC_ENTRY_PLAIN, LC_ENTRY_INT8, LC_ENTRY_FP8, LC_ENTRY_FP4 = -1, 0, 1, 2
 
 
+def fits(names: str, *values) -> None:
+    """ctypes would cut off the high bits of integers that do not fit into fields of 32 bits (of 64: give the value >> 32)."""
+    if max(values) >> 31 > 0 or min(values) >> 31 < -1:
+        name = next(n for n, v in zip(names.split(), values) if v >> 31 not in (0, -1))
+        raise ValueError(f"{name} does not fit into the library's integers")
+
+
 class lc_strides(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("batch", "token", "head")]
 
@@ -753,6 +760,7 @@ def make_dit_options(entry: Optional[str] = None, keep: int = 0, block: int = 64
     formats = {None: LC_ENTRY_PLAIN, "mxint8": LC_ENTRY_INT8, "mxfp8": LC_ENTRY_FP8, "mxfp4": LC_ENTRY_FP4}
     if entry not in formats:
         raise ValueError("entry must be None, mxint8, mxfp8 or mxfp4")
+    fits("keep block q_block sink window grid", keep, block, q_block, sink, window, max(grid or [0], key=abs))
     return lc_dit_options(entry_format=formats[entry], keep=keep, block=block, q_block=q_block, sink=sink, window=window,
                           rope=None if rope is None else C.pointer(rope), grid=(C.c_int32 * 3)(*(grid or [])))
 

@@ -97,6 +97,7 @@ def make_rope(head_dim: int, axes: Optional[Sequence[int]] = None, base: float =
     dims = [head_dim] if axes is None else list(axes)
     if not 1 <= len(dims) <= 3:
         raise ValueError("there are one to three axes")
+    lcb.fits("head_dim orig_len axes", head_dim, orig_len, max(dims))
     return lcb.lc_rope_make(lcb.lc_rope_config(head_dim=head_dim, axes=len(dims), axis_dim=(lcb.C.c_int32 * 3)(*dims),
                                                layout=_named(LAYOUTS, "layout", layout), scaling=_named(SCALINGS, "scaling", scaling),
                                                orig_len=orig_len, base=base, factor=factor, beta_fast=beta_fast, beta_slow=beta_slow))
@@ -134,7 +135,9 @@ def _rope_args(shape, x_stride, y_stride, dtype, n, grid, starts, inverse, pos_b
     if len(starts) != n or (grid is not None and len(grid) != n):
         raise ValueError(f"grid and start have one value for each of the {n} axes")
     xs = _strides("x", shape, x_stride)
-    return lcb.lc_rope_args(B=shape[0], T=shape[1], heads=shape[2], dtype=_dtype("x", dtype), x=xs, y=_strides("out", shape, y_stride),
+    lcb.fits("T grid start", max(shape), max(grid or (0,), key=abs), max(starts, key=abs) >> 32)
+    ys = xs if y_stride == x_stride else _strides("out", shape, y_stride)
+    return lcb.lc_rope_args(B=shape[0], T=shape[1], heads=shape[2], dtype=_dtype("x", dtype), x=xs, y=ys,
                             inverse=int(inverse), grid=(lcb.C.c_int32 * 3)(*(grid or ())), start=(lcb.C.c_int64 * 3)(*starts),
                             pos_batch=pos_batch)
 
@@ -146,6 +149,7 @@ def block_means(k, block: int = 64, k_len=None, first: int = 0, count: Optional[
     a, nk = _means_args(k.shape, k.stride(), k.dtype, block)
     B, Tk, Hkv, d = k.shape
     count = nk - first if count is None else count
+    lcb.fits("first count", first, count)
     if out is None and (first, count) != (0, nk):
         raise ValueError("some blocks of a tensor: give the tensor")
     _on(k.device, k_len, out)
@@ -160,6 +164,7 @@ def block_means(k, block: int = 64, k_len=None, first: int = 0, count: Optional[
 def _means_args(shape, stride, dtype, block):
     s = _strides("k", shape, stride)
     B, Tk, Hkv, d = shape
+    lcb.fits("Tk block", max(shape), block)
     a = lcb.lc_sparse_args(B=B, Tq=1, Tk=Tk, heads=Hkv, kv_heads=Hkv, head_dim=d, dtype=_dtype("k", dtype), block=block, q_block=1, keep=1,
                            window=-1, k=s)
     return a, lcb.lc_sparse_blocks(a)
@@ -188,6 +193,7 @@ def _select_args(shape, stride, dtype, m_shape, Tk, keep, block, q_block, sink, 
     B, Tq, H, d = shape
     if len(m_shape) != 4 or m_shape[0] != B or m_shape[2] != d:
         raise ValueError("means must be what block_means made for these sizes")
+    lcb.fits("Tq Tk keep block q_block sink window q_pos0", max(shape), Tk, keep, block, q_block, sink, window, q_pos0 >> 32)
     a = lcb.lc_sparse_args(B=B, Tq=Tq, Tk=Tk, heads=H, kv_heads=m_shape[1], head_dim=d, dtype=_dtype("q", dtype), block=block,
                            q_block=q_block, keep=keep, sink=sink, window=window, q_pos0=q_pos0, q=s)
     if m_shape[3] != lcb.lc_sparse_blocks(a):
@@ -215,10 +221,12 @@ def block_attention(q, k, v, index, block: int = 64, q_block: int = 128, q_len=N
 
 @_kept
 def _attention_args(q_shape, q_stride, dtype, k_shape, k_stride, v_shape, v_stride, out_stride, index_shape, block, q_block, q_prescaled):
-    sq, sk, sv = _strides("q", q_shape, q_stride), _strides("k", k_shape, k_stride), _strides("v", v_shape, v_stride)
+    sq, sk = _strides("q", q_shape, q_stride), _strides("k", k_shape, k_stride)
+    sv = sk if (v_shape, v_stride) == (k_shape, k_stride) else _strides("v", v_shape, v_stride)
     B, Tq, H, d = q_shape
     if k_shape != v_shape or k_shape[0] != B or k_shape[3] != d:
         raise ValueError("k and v must be [B, Tk, kv_heads, head_dim] of q's batch and head_dim")
+    lcb.fits("Tq Tk keep block q_block", max(q_shape), max(k_shape), max(index_shape), block, q_block)
     a = lcb.lc_sparse_args(B=B, Tq=Tq, Tk=k_shape[1], heads=H, kv_heads=k_shape[2], head_dim=d, dtype=_dtype("q", dtype), block=block,
                            q_block=q_block, keep=index_shape[3] if len(index_shape) == 4 else 0, window=-1, q_prescaled=int(q_prescaled),
                            q=sq, k=sk, v=sv, out=_strides("out", q_shape, out_stride))
@@ -228,6 +236,7 @@ def _attention_args(q_shape, q_stride, dtype, k_shape, k_stride, v_shape, v_stri
 # ---- quantised cache entries ------------------------------------------------------------------------------------------
 def entry_bytes(rows: int, cols: int, fmt: str) -> int:
     """Bytes of an entry of rows x cols values."""
+    lcb.fits("rows cols", rows >> 32, cols)
     return lcb.lc_entry_packed_bytes(lcb.lc_entry_args(format=_named(FORMATS, "fmt", fmt), rows=rows, cols=cols))
 
 
@@ -281,6 +290,7 @@ def _entry_args(fmt, shape, x_stride, x_dtype, y_shape, y_stride, y_dtype):
     if x_stride is not None:
         a.x_ld, a.x_dtype = _row_stride("x", shape, x_stride), _dtype("x", x_dtype)
     a.rows, a.cols = shape
+    lcb.fits("cols", shape[1])
     if y_shape is not None:
         if tuple(y_shape) != tuple(shape):
             raise ValueError(f"out must be of shape {tuple(shape)}")

@@ -2,6 +2,7 @@
 import math
 
 import pytest
+import torch
 
 from paper_2510_05367_amd import binding as lcb
 from paper_2510_05367_amd import tokens
@@ -28,3 +29,25 @@ def test_rope_tables_of_wide_factors(scaling, dim, factor):
             keep = min(max((4096 * w / (2 * math.pi) - 1) / 31, 0), 1)
             w *= keep + (1 - keep) / factor
         assert t.turns[i] == pytest.approx(w / (2 * math.pi), rel=1e-12)
+
+
+def test_numbers_that_do_not_fit_are_refused():
+    """None is cut to its low bits: a window of 2^63 - 1 blocks would be -1, none."""
+    x, m, t = torch.zeros(1, 4, 2, 64), torch.zeros(1, 2, 64, 1, dtype=torch.float64), tokens.make_rope(64)
+    far = 2 ** 32
+    for name, bad in (("window", lambda: tokens.block_select(x, m, 4, 1, window=2 ** 63 - 1)), ("sink", lambda: tokens.block_select(x, m, 4, 1, sink=far)),
+                      ("keep", lambda: tokens.block_select(x, m, 4, far + 1)), ("q_block", lambda: tokens.block_select(x, m, 4, 1, q_block=far + 1)),
+                      ("Tk", lambda: tokens.block_select(x, m, far + 4, 1)), ("q_pos0", lambda: tokens.block_select(x, m, 4, 1, q_pos0=2 ** 64)),
+                      ("block", lambda: tokens.block_means(x, block=far + 64)), ("first", lambda: tokens.block_means(x, first=far, count=1, out=m)),
+                      ("start", lambda: tokens.rope(x, t, start=2 ** 64 + 5)), ("T ", lambda: tokens.rope(x[:, :1].expand(1, far + 4, 2, 64), t, out=x[:, :1].expand(1, far + 4, 2, 64))),
+                      ("grid", lambda: tokens.rope(x, tokens.make_rope(64, axes=(32, 32)), grid=(2, far + 2))),
+                      ("axes", lambda: tokens.make_rope(64, axes=(far + 64,))), ("orig_len", lambda: tokens.make_rope(64, scaling="parts", factor=2.0, orig_len=far + 64)),
+                      ("head_dim", lambda: tokens.make_rope(far + 64, axes=(64,))), ("cols", lambda: tokens.entry_bytes(1, far + 32, "mxint8")),
+                      ("block", lambda: tokens._attention_args(*[x.shape, x.stride(), x.dtype] + [x.shape, x.stride()] * 2 + [x.stride(), (1, 2, 1, 1), far + 64, 1, False])),
+                      ("Tk", lambda: tokens.block_means(x[:, :1].expand(1, far + 4, 2, 64))),
+                      ("cols", lambda: tokens._entry_args("mxint8", (1, far + 32), None, None, (1, far + 32), (0, 1), torch.float32)),
+                      ("rows", lambda: tokens.entry_bytes(2 ** 64 + 1, 32, "mxint8")), ("keep", lambda: lcb.make_dit_options(keep=far + 1)),
+                      ("window", lambda: lcb.make_dit_options(window=2 ** 63 - 1)), ("grid", lambda: lcb.make_dit_options(grid=(far + 1, 1, 1)))):
+        with pytest.raises(ValueError, match=name):
+            bad()
+    assert lcb.make_dit_options(window=2 ** 31 - 1).window == 2 ** 31 - 1
