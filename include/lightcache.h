@@ -574,8 +574,9 @@ typedef struct lc_rope_args {
   int64_t pos_batch;       /* with pos: elements from one batch element's positions to the next's, 0 = shared */
 } lc_rope_args;
 /* y = rotated x. pos [device, int32, .. T x axes] or NULL: the positions, where they are not the cells of a grid. y may be x
- * (with its strides); otherwise the two must not overlap. Any strides and alignment are taken; heads of whole 16-byte packets, 16-byte
- * aligned, move in packets. */
+ * (with its strides); otherwise the two must not overlap. Any strides and alignment are taken. Rows move in packets of several channels
+ * where they are aligned to those and every axis (and the channels behind the pairs, unless in place) is made of whole ones: axis_dim / 2 a
+ * multiple of 4 (LC_ROPE_HALF, and LC_ROPE_INTERLEAVED in bf16) or of 2 (interleaved float); channel by channel otherwise. */
 lc_status lc_op_rope(const lc_rope_table* table /* [host] */, const lc_rope_args* args /* [host] */, const void* x, const int32_t* pos,
                      void* y, void* stream);
 
@@ -599,7 +600,9 @@ int32_t lc_sparse_groups(const lc_sparse_args* args); /* groups of queries: ceil
 int32_t lc_sparse_blocks(const lc_sparse_args* args); /* blocks of keys: ceil(Tk / block) */
 /* means[b][kv head][channel][block] = mean of the block's existing keys (0 where none exists), for the blocks [first, first +
  * count): a cache that grows has only its last blocks done again. [device, double, B x kv_heads x head_dim x lc_sparse_blocks].
- * Kept in 64 bits, as the scores are: the order of two blocks then depends on the keys, not on the order of a sum. */
+ * Kept in 64 bits, as the scores and the sums behind both are, so that the order of two blocks depends on the keys and not on the order of a
+ * sum: sums of 128 bf16 numbers within 2^38 of each other are exact, and others lose 2^-53 at a time. (Scores that differ by no
+ * more than that may change places between calls of other sizes, which sum their queries in another order.) */
 lc_status lc_op_block_means(const lc_sparse_args* args, const void* k, const int32_t* k_len, double* means, int first, int count,
                             void* stream);
 /* index[b][head][group][keep] [device, int32]: the group's blocks, ascending, -1 behind the last. Blocks without an existing key are
@@ -609,7 +612,9 @@ lc_status lc_op_block_select(const lc_sparse_args* args, const void* q, const do
                              int32_t* index, void* stream);
 /* out[b][i][h] = softmax(q_i K^T / sqrt(head_dim)) V over the existing keys of the blocks in index[b][h][i / q_block]; zeros where
  * there are none. A list ends at its first entry that is not a block with an existing key or not greater than the entry
- * before it, so that lists of any origin are safe and no key counts twice. out must not overlap the inputs. workspace [device, 16-byte aligned], of
+ * before it, so that lists of any origin are safe and no key counts twice. Scores, statistics and sums are fp32; bf16 calls round the
+ * probabilities to bf16 before they meet V, alike in numerator and denominator. Calls of other sizes may sum in another order.
+ * out must not overlap the inputs. workspace [device, 16-byte aligned], of
  * lc_block_attention_workspace(args) bytes (0: may be NULL): what several workgroups that share a list hand to each other; calls in
  * flight at once need one each. */
 size_t lc_block_attention_workspace(const lc_sparse_args* args); /* host only; 0 also if args are refused */

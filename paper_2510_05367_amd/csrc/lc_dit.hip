@@ -385,8 +385,8 @@ lc_status run_block(lc_dit* c, int i, const float* mod, float* x, const float* d
   // The chunk bounds the memory, and a pass takes as many rows as there is memory for: what is held for all tokens is not
   // needed all the time. The normalised rows of q,k,v lie where the attention output will be, the branch output (where it
   // exists) where q,k,v were, and the MLP works from q,k,v to the end of the arena, which holds all rows of it whatever the chunk
-  // in bf16 stages with fused gated sums and mlp_ratio up to 4: 10 D bytes a row, of which q,k,v, V^T and attention output have
-  // that much; without the fusion it takes 14 D. (2 x 3108 tokens of 1024 in chunks of 1024, us a block's linear layers: 403 in
+  // in bf16 stages with fused gated sums, mlp_ratio up to 4 and attention over all tokens: 10 D bytes a row, of which q,k,v, V^T and attention
+  // output have that much (with selected blocks there is no V^T: 8 D, the means and the lists); without the fusion it takes 14 D. (2 x 3108 tokens of 1024 in chunks of 1024, us a block's linear layers: 403 in
   // launches of 1024 rows, 213.)
   // ---- attention branch: q,k,v of every token first
   if ((s = ln_mod(c, x, delta, m, 0, 1, ao, (int)R, 0)) != LC_OK) return s;

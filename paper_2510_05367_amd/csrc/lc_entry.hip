@@ -119,6 +119,8 @@ template <int F> __device__ __forceinline__ uint32_t get_codes(const unsigned ch
 
 // A thread holds four values of a row, eight neighbouring threads a group. Rows are cut into ppr = 8 * groups packets of four. Bound by
 // the bytes: 8192 x 1024 floats to 8-bit codes with a sum 21.4 us = 5.1 TB/s (a large copy 5.2), 33001 x 1000 bf16 to 4 bits with a float sum 68.8 us = 5.1.
+// Rows that are not whole aligned packets load and store value by value: 8192 x 1024 floats, with a sum, in rows of 1024 and of 1025 16.6 and 25.2 us, read back
+// with a sum 12.8 and 18.8 (partly out of the last-level cache).
 template <int F, class X, class Y, bool WHOLE>
 __global__ __launch_bounds__(256) void entry_pack_kernel(const X* x, int64_t x_ld, unsigned char* __restrict__ codes,
                                                          unsigned char* __restrict__ scales, const Y* base, Y* y, int64_t y_ld,

@@ -4,7 +4,8 @@ cache entries (the C ABI's section of the same name in include/lightcache.h, whi
 Tensors are [B, T, heads, head_dim] views of any strides with channels next to each other (rows of packed q,k,v, say). Calls
 enqueue on torch's current stream of the tensors' device and take outputs and workspaces from torch's allocator on it, so
 they order with torch's own work and may be captured into a graph. No gradients are recorded (the map of :func:`rope` has its
-transpose: ``inverse=True``). What a call refuses raises :class:`binding.LcError`, or ``ValueError`` where it never gets there.
+transpose: ``inverse=True``). Formats of entries are the C ABI's: "mxfp8" and "mxfp4" groups hold what such groups commonly do (e4m3 and
+e2m1 codes, scale bytes of exponent + 127), "mxint8" codes count ones, where the published format of that name counts 2^-6. What a call refuses raises :class:`binding.LcError`, or ``ValueError`` where it never gets there.
 """
 from __future__ import annotations
 
@@ -85,7 +86,8 @@ def _out(out, shape, dtype, device, name="out"):
 
 
 # Descriptors depend on shapes, strides, types and options alone: those of the last few hundred kinds of call are kept, so that a
-# call does not pay for making one (10 us of the 20 that a call of this layer took).
+# repeated call does not pay for making one. A position, an offset or a length that moves from call to call is one of those options: such
+# calls make theirs each time (us of the host, repeated and moving: rope 6.2 and 8.3, block_select 6.1 and 8.5, block_attention 14.2 and 17.8).
 _kept = functools.lru_cache(maxsize=512)
 
 
