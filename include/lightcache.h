@@ -574,7 +574,7 @@ typedef struct lc_rope_args {
   int64_t pos_batch;       /* with pos: elements from one batch element's positions to the next's, 0 = shared */
 } lc_rope_args;
 /* y = rotated x. pos [device, int32, .. T x axes] or NULL: the positions, where they are not the cells of a grid. y may be x
- * (with its strides); otherwise the two must not overlap. Any strides and alignment are taken. Rows move in packets of several channels
+ * (with its strides); otherwise the two must not overlap. B at most 65535, T 2^27, heads 2^20. Any strides and alignment are taken. Rows move in packets of several channels
  * where they are aligned to those and every axis (and the channels behind the pairs, unless in place) is made of whole ones: axis_dim / 2 a
  * multiple of 4 (LC_ROPE_HALF, and LC_ROPE_INTERLEAVED in bf16) or of 2 (interleaved float); channel by channel otherwise. */
 lc_status lc_op_rope(const lc_rope_table* table /* [host] */, const lc_rope_args* args /* [host] */, const void* x, const int32_t* pos,
@@ -585,7 +585,8 @@ lc_status lc_op_rope(const lc_rope_table* table /* [host] */, const lc_rope_args
  * the group's queries and of the block's keys; a list holds the `keep` blocks of the highest scores. Query head h reads key
  * head h / (heads / kv_heads).
  * Requirements (else LC_ERR_SHAPE): sizes > 0; heads a multiple of kv_heads; head_dim in {8, 16, 32, 40, 64, 128}; block a
- * multiple of 64, at most 2^20; 1 <= q_block <= 128; keep <= 65536; Tk <= 2^30; at most 8192 blocks; strides and pointers of q, k, v and out such that every
+ * multiple of 64, at most 2^20; 1 <= q_block <= 128; keep <= 65536; Tk <= 2^30; at most 8192 blocks; at most 2^24 heads and 2^22 groups of queries of all
+ * heads and batch elements (selections of several groups a workgroup and attention take more); means of at most 2^25 blocks at a time, each head's counted in fours; |q_pos0| <= 2^40; strides and pointers of q, k, v and out such that every
  * head's row is 16-byte aligned; attention to more than one key: token strides of k and v at least head_dim, 64 of them within 2^30 bytes. */
 typedef struct lc_sparse_args {
   int32_t B, Tq, Tk, heads, kv_heads, head_dim, dtype;
